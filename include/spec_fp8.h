@@ -460,6 +460,110 @@ spec_status spec_verify_accept_tree(const void* target_logits, const int32_t* pa
 spec_status spec_tree_attention_mask(const int32_t* parents, int64_t B, int64_t N, uint64_t* mask, int32_t* depth,
                                      void* stream);
 
+/*
+ * spec_fp8_kv_cache_read -- rows of the paged FP8 KV cache back as bf16: what
+ * spec_fp8_kv_cache_write stored (section 3.2), for programs that move or
+ * recompute with cached keys and values.  For every token t < T with slot
+ * s = slot_mapping[t] in [0, num_slots) and every KV head h < H:
+ *
+ *   k[t*ld_k + h*D + d] = bf16_RNE(fl32(dec(k_cache[(s*H + h)*D + d]) * sk))
+ *                         sk = k_scale[s*H + h] (PER_ROW) or k_scale[0] (PER_TENSOR)
+ *
+ * and v likewise.  A token whose slot is negative (padding) or >= num_slots
+ * reads as zeros.  NaN codes give NaN.  A slot may be read any number of times.
+ *
+ * k_cache, v_cache, k_scale, v_scale, slot_mapping, H, D, num_slots, mode: as
+ *            spec_fp8_kv_cache_write; all read here.
+ * k, v       bf16 [T, ld_k] / [T, ld_v]; head h at columns [h*D, (h+1)*D), the other
+ *            columns keep their contents.
+ * Requirements: those of spec_fp8_kv_cache_write.  num_slots == 0 reads zeros.
+ */
+spec_status spec_fp8_kv_cache_read(const uint8_t* k_cache, const uint8_t* v_cache, const float* k_scale,
+                                   const float* v_scale, spec_scale_mode mode, const int64_t* slot_mapping, int64_t T,
+                                   int64_t H, int64_t D, int64_t num_slots, void* k, int64_t ld_k, void* v,
+                                   int64_t ld_v, void* stream);
+
+/*
+ * spec_fp8_paged_attention -- attention of new tokens over the paged FP8 KV
+ * cache: the target's scoring pass over drafted chains (B*(k+1) rows, section
+ * 3.1), over drafted trees (tree attention), of single generated tokens, and
+ * of the next chunk of a long prompt.
+ *
+ * Sequence b has n_b new rows of q and L_b = kv_lens[b] tokens in the cache,
+ * those of the new rows included and last (written before this call).  Its
+ * j-th token lies in slot block_tables[b*ld_tables + j / block_size] * block_size
+ * + j % block_size; a token whose table entry is outside [0, num_blocks) is not
+ * there: no row sees it.  Query head g reads KV head g / (Hq/H).  Row i sees
+ *
+ *   chain: token j iff j <= L_b - n_b + i;
+ *   tree:  the prefix and the root (j < L_b - N), and node m (j = L_b - N + m) iff
+ *          i >= 1 and bit m of tree_mask[b*N + i-1] is set: row 0 is the root's, row
+ *          i the row of node i-1, n_b = N + 1.
+ *
+ *   s_ij   = scale * sum_d q[i,d] * dec(K[j,d]) * sk_j
+ *   out[i] = bf16_RNE( sum_j p_ij dec(V[j]) sv_j / sum_j p_ij ),  p_ij = 2^(log2(e) (s_ij - m_i))
+ *
+ * over the tokens seen (m_i: a reference within 2^8 of the largest s_ij); a row that sees none, or only scores
+ * of -inf, is zeros.  What a row does not see has no influence on it, NaN codes and scales
+ * included.  Products of q and codes are exact; they are summed, and the sums
+ * of p and p*v accumulated, in fp32; p_ij * sv_j is rounded to bf16 (to nearest)
+ * for the second product.
+ *
+ * q        bf16 [T, ld_q], head h at columns [h*D, (h+1)*D).  The rows of sequence b are
+ *          cu_q[b] .. cu_q[b+1]-1, or with cu_q NULL T/B rows each (T % B == 0,
+ *          SPEC_ERR_SHAPE).  cu_q int32 [B+1], not decreasing, 0 <= cu_q <= T; rows outside
+ *          [cu_q[0], cu_q[B]) are left as they were in out.
+ * k_cache, v_cache  uint8 [num_blocks*block_size, H, D]; k_scale, v_scale fp32
+ *          [num_blocks*block_size, H] (PER_ROW) or [1] (PER_TENSOR), as
+ *          spec_fp8_kv_cache_write leaves them.
+ * block_tables int32 [B, ld_tables], max_blocks <= ld_tables entries each; kv_lens int32 [B]
+ *          (< 0 counts as 0, beyond max_blocks*block_size as that).
+ * tree_mask uint64 [B, N] of spec_tree_attention_mask, or NULL with N = 0.  With a tree cu_q
+ *          is NULL and T = B*(N+1) (SPEC_ERR_SHAPE), 1 <= N <= 64 (SPEC_ERR_UNSUPPORTED above).
+ * out      bf16 [T, ld_out]; may not overlap q.
+ * workspace  >= spec_fp8_paged_attention_workspace_bytes(T, B, Hq, H, D) bytes, 16-byte
+ *          aligned (SPEC_ERR_WORKSPACE, SPEC_ERR_ALIGN).  Its first 16 KiB hold tickets: zero
+ *          before the first call that uses it (fill it with zeros once), left zero
+ *          by every call, whatever its shape.  Calls that share a workspace must not
+ *          overlap.
+ * Requirements: T, B >= 0 (0: no-op), Hq, H, D, block_size > 0, max_blocks, num_blocks >= 0,
+ * Hq % H == 0, ld_q and ld_out >= Hq*D, ld_tables >= max_blocks (SPEC_ERR_SHAPE); D % 8 == 0,
+ * D <= 256, Hq <= 65535, T*Hq, B, num_blocks and max_blocks*block_size < 2^31 (SPEC_ERR_UNSUPPORTED); q, out,
+ * k_cache and v_cache 16-byte aligned, ld_q and ld_out multiples of 8, tree_mask 8-byte, the
+ * tables, lengths and scales 4-byte aligned (SPEC_ERR_ALIGN); scale finite and > 0
+ * (SPEC_ERR_VALUE); mode PER_ROW or PER_TENSOR (SPEC_ERR_ENUM).
+ */
+size_t spec_fp8_paged_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D);
+
+spec_status spec_fp8_paged_attention(const void* q, int64_t ld_q, const uint8_t* k_cache, const uint8_t* v_cache,
+                                     const float* k_scale, const float* v_scale, spec_scale_mode mode,
+                                     const int32_t* block_tables, int64_t ld_tables, int64_t max_blocks,
+                                     const int32_t* kv_lens, const int32_t* cu_q, const uint64_t* tree_mask,
+                                     int64_t N, int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D,
+                                     int64_t block_size, int64_t num_blocks, float scale, void* out, int64_t ld_out,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * spec_prompt_attention_bf16 -- causal attention over B whole prompts packed
+ * one after the other (the prefill that fills the cache): row i of a prompt
+ * sees its rows 0..i.  Scores, reference and sums as spec_fp8_paged_attention,
+ * with bf16 keys and values and p_ij rounded to bf16 for the second product.
+ *
+ * q  bf16 [T, ld_q], Hq heads of D; k, v bf16 [T, ld_k] / [T, ld_v], H heads of D: the column
+ *    blocks of the QKV projection's output fit directly.  Query head g reads KV head g / (Hq/H).
+ * cu_seqlens int32 [B+1], not decreasing, 0 <= cu_seqlens <= T: prompt b is rows cu_seqlens[b]
+ *    .. cu_seqlens[b+1]-1 (none: an empty prompt).  Rows outside [cu_seqlens[0],
+ *    cu_seqlens[B]) are neither read nor written.
+ * out bf16 [T, ld_out]; may not overlap the inputs.
+ * Requirements: T, B >= 0 (0: no-op), Hq, H, D > 0, Hq % H == 0, ld_q, ld_out >= Hq*D, ld_k,
+ * ld_v >= H*D (SPEC_ERR_SHAPE); D % 8 == 0, D <= 256, Hq <= 65535, T*Hq and B < 2^31 (SPEC_ERR_UNSUPPORTED);
+ * all tensors 16-byte aligned with strides that are multiples of 8, cu_seqlens 4-byte aligned
+ * (SPEC_ERR_ALIGN); scale finite and > 0 (SPEC_ERR_VALUE).  No workspace.
+ */
+spec_status spec_prompt_attention_bf16(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v,
+                                       int64_t ld_v, const int32_t* cu_seqlens, int64_t T, int64_t B, int64_t Hq,
+                                       int64_t H, int64_t D, float scale, void* out, int64_t ld_out, void* stream);
+
 /* Static description of a status code (never NULL). */
 const char* spec_status_string(spec_status s);
 

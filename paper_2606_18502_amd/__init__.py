@@ -37,6 +37,10 @@ from .ops import (  # noqa: F401
     clip_count,
     silu_mul,
     kv_cache_write,
+    kv_cache_read,
+    paged_attention,
+    paged_attention_workspace_bytes,
+    prompt_attention,
     gemm,
     gemm_workspace_bytes,
     gemm_logit_stats,

@@ -23,6 +23,8 @@ EXPORTS = ("spec_fp8_quantize", "spec_silu_mul_bf16", "spec_fp8_kv_cache_write",
            "spec_verify_accept_workspace_bytes", "spec_verify_accept", "spec_verify_accept_noalloc",
            "spec_verify_accept_stats",
            "spec_verify_accept_tree_workspace_bytes", "spec_verify_accept_tree", "spec_tree_attention_mask",
+           "spec_fp8_kv_cache_read", "spec_fp8_paged_attention_workspace_bytes", "spec_fp8_paged_attention",
+           "spec_prompt_attention_bf16",
            "spec_status_string", "spec_last_hip_error", "spec_version")
 
 _lib = None
@@ -60,6 +62,15 @@ def declare(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.spec_fp8_clip_count.restype = i32
     lib.spec_fp8_kv_cache_write.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, i64, i32, vp, vp, vp, vp, vp]
     lib.spec_fp8_kv_cache_write.restype = i32
+    lib.spec_fp8_kv_cache_read.argtypes = [vp, vp, vp, vp, i32, vp, i64, i64, i64, i64, vp, i64, vp, i64, vp]
+    lib.spec_fp8_kv_cache_read.restype = i32
+    lib.spec_fp8_paged_attention_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
+    lib.spec_fp8_paged_attention_workspace_bytes.restype = sz
+    lib.spec_fp8_paged_attention.argtypes = [vp, i64, vp, vp, vp, vp, i32, vp, i64, i64, vp, vp, vp, i64, i64, i64, i64,
+                                             i64, i64, i64, i64, f32, vp, i64, vp, sz, vp]
+    lib.spec_fp8_paged_attention.restype = i32
+    lib.spec_prompt_attention_bf16.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i64, i64, i64, i64, f32, vp, i64, vp]
+    lib.spec_prompt_attention_bf16.restype = i32
     lib.spec_fp8_gemm_workspace_bytes.argtypes = [i64, i64, i64]
     lib.spec_fp8_gemm_workspace_bytes.restype = sz
     lib.spec_fp8_gemm.argtypes = [vp, i64, vp, i32, vp, i64, vp, i32, i64, i64, i64, vp, i64, i32, vp, sz, vp]

@@ -33,7 +33,7 @@ ARCH = "gfx950"
 
 # longest compiles first: they run in parallel
 HIP_SOURCES = ["gemm_k0_1.hip", "gemm_k2_3.hip", "gemm_k4_6.hip", "gemm_k7_12.hip", "accept.hip", "quantize.hip",
-               "gemm.hip", "kvcache.hip", "tree_mask.hip", "api.cpp", "plan.cpp"]
+               "gemm.hip", "kvcache.hip", "attention.hip", "api.cpp", "plan.cpp"]
 HOST_SOURCES = ["validate.cpp"]
 BIND_SOURCE = "torch_bind.cpp"
 BIND = os.path.join(HERE, "_torch_bind.so")

@@ -67,6 +67,94 @@ spec_status spec_fp8_kv_cache_write(const void* k, int64_t ld_k, const void* v, 
         as_stream(stream)));
 }
 
+spec_status spec_fp8_kv_cache_read(const uint8_t* k_cache, const uint8_t* v_cache, const float* k_scale,
+                                   const float* v_scale, spec_scale_mode mode, const int64_t* slot_mapping, int64_t T,
+                                   int64_t H, int64_t D, int64_t num_slots, void* k, int64_t ld_k, void* v,
+                                   int64_t ld_v, void* stream) {
+    const spec_status st = specfp8::check_kv_cache_read(k_cache, v_cache, k_scale, v_scale, (int)mode, slot_mapping, T,
+                                                        H, D, num_slots, k, ld_k, v, ld_v);
+    if (st != SPEC_OK || T == 0) return st;
+    if (!specfp8::launch_kv_cache_read) return from_hip(hipErrorNotSupported);
+    return from_hip(specfp8::launch_kv_cache_read(
+        k_cache, v_cache, k_scale, v_scale, mode == SPEC_SCALE_PER_TENSOR ? 1 : 0, slot_mapping, T, H, D, num_slots,
+        reinterpret_cast<uint16_t*>(k), ld_k, reinterpret_cast<uint16_t*>(v), ld_v, as_stream(stream)));
+}
+
+size_t spec_fp8_paged_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D) {
+    if (T <= 0 || B <= 0 || Hq <= 0 || H <= 0 || D <= 0 || Hq % H != 0 || D > 256 || T > 2147483647LL / Hq) return 0;
+    return specfp8::paged_attention_workspace_bytes(T, B, Hq, H, D);
+}
+
+spec_status spec_fp8_paged_attention(const void* q, int64_t ld_q, const uint8_t* k_cache, const uint8_t* v_cache,
+                                     const float* k_scale, const float* v_scale, spec_scale_mode mode,
+                                     const int32_t* block_tables, int64_t ld_tables, int64_t max_blocks,
+                                     const int32_t* kv_lens, const int32_t* cu_q, const uint64_t* tree_mask,
+                                     int64_t N, int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D,
+                                     int64_t block_size, int64_t num_blocks, float scale, void* out, int64_t ld_out,
+                                     void* workspace, size_t workspace_bytes, void* stream) {
+    const spec_status st = specfp8::check_paged_attention(q, ld_q, k_cache, v_cache, k_scale, v_scale, (int)mode,
+                                                          block_tables, ld_tables, max_blocks, kv_lens, cu_q,
+                                                          tree_mask, N, T, B, Hq, H, D, block_size, num_blocks, scale,
+                                                          out, ld_out);
+    if (st != SPEC_OK || T == 0 || B == 0) return st;
+    if (!workspace || workspace_bytes < specfp8::paged_attention_workspace_bytes(T, B, Hq, H, D))
+        return SPEC_ERR_WORKSPACE;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 15u) != 0) return SPEC_ERR_ALIGN;
+    specfp8::PagedArgs a;
+    a.q = reinterpret_cast<const uint16_t*>(q);
+    a.k_cache = k_cache;
+    a.v_cache = v_cache;
+    a.k_scale = k_scale;
+    a.v_scale = v_scale;
+    a.tables = block_tables;
+    a.kv_lens = kv_lens;
+    a.cu_q = cu_q;
+    a.tree = tree_mask;
+    a.out = reinterpret_cast<uint16_t*>(out);
+    a.ld_q = ld_q;
+    a.ld_out = ld_out;
+    a.ld_tables = ld_tables;
+    a.T = (int32_t)T;
+    a.B = (int32_t)B;
+    a.N = (int32_t)N;
+    a.Hq = (int32_t)Hq;
+    a.H = (int32_t)H;
+    a.D = (int32_t)D;
+    a.block_size = (int32_t)block_size;
+    a.num_blocks = (int32_t)num_blocks;
+    a.max_len = (int32_t)(max_blocks * block_size);
+    a.per_tensor = mode == SPEC_SCALE_PER_TENSOR ? 1 : 0;
+    a.scale = scale;
+    if (!specfp8::launch_paged_attention) return from_hip(hipErrorNotSupported);
+    return from_hip(specfp8::launch_paged_attention(a, workspace, as_stream(stream)));
+}
+
+spec_status spec_prompt_attention_bf16(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v,
+                                       int64_t ld_v, const int32_t* cu_seqlens, int64_t T, int64_t B, int64_t Hq,
+                                       int64_t H, int64_t D, float scale, void* out, int64_t ld_out, void* stream) {
+    const spec_status st = specfp8::check_prompt_attention(q, ld_q, k, ld_k, v, ld_v, cu_seqlens, T, B, Hq, H, D,
+                                                           scale, out, ld_out);
+    if (st != SPEC_OK || T == 0 || B == 0) return st;
+    specfp8::PromptArgs a;
+    a.q = reinterpret_cast<const uint16_t*>(q);
+    a.k = reinterpret_cast<const uint16_t*>(k);
+    a.v = reinterpret_cast<const uint16_t*>(v);
+    a.cu = cu_seqlens;
+    a.out = reinterpret_cast<uint16_t*>(out);
+    a.ld_q = ld_q;
+    a.ld_k = ld_k;
+    a.ld_v = ld_v;
+    a.ld_out = ld_out;
+    a.T = (int32_t)T;
+    a.B = (int32_t)B;
+    a.Hq = (int32_t)Hq;
+    a.H = (int32_t)H;
+    a.D = (int32_t)D;
+    a.scale = scale;
+    if (!specfp8::launch_prompt_attention) return from_hip(hipErrorNotSupported);
+    return from_hip(specfp8::launch_prompt_attention(a, as_stream(stream)));
+}
+
 size_t spec_fp8_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K) {
     if (M <= 0 || N <= 0 || K <= 0 || K % 128 != 0) return 0;
     return specfp8::plan_gemm(M, N, K).workspace_bytes;

@@ -1,0 +1,202 @@
+// Tree attention masks for token-tree verification: for every node of a
+// drafted tree, the set of tree nodes its row may attend to (the nodes on the
+// path from the root to it, itself included) as a 64-bit mask, and its depth.
+//
+// One wave per sequence, lane n owning node n (N <= 64).  The masks come from
+// pointer jumping over the parent links: after step s every lane holds the
+// nodes within 2^s - 1 steps above it and a pointer to its 2^s-th ancestor,
+// so six steps of lane exchanges (no memory traffic) cover any depth up to
+// 64.  A node whose parent is not one of the earlier nodes (or -1) poisons
+// itself and, through the same exchanges, every node below it.
+#include "device_common.hpp"
+#include "kernels.hpp"
+
+namespace specfp8 {
+
+namespace {
+
+constexpr int kTmThreads = 256;
+constexpr int kTmSeqPerBlock = kTmThreads / 64;
+
+__global__ __launch_bounds__(kTmThreads) void tree_mask_kernel(const int32_t* __restrict__ parents, int64_t B,
+                                                               int N, uint64_t* __restrict__ mask,
+                                                               int32_t* __restrict__ depth) {
+    const int lane = threadIdx.x & 63;
+    const int64_t b = (int64_t)blockIdx.x * kTmSeqPerBlock + threadIdx.x / 64;   // wave-uniform
+    if (b >= B) return;
+    const bool node = lane < N;
+    const int p = node ? parents[b * N + lane] : -1;
+    int bad = (node && (p < -1 || p >= lane)) ? 1 : 0;
+    uint32_t lo = 0, hi = 0;                  // the mask, as two halves for the lane exchanges
+    if (node) {
+        if (lane < 32) lo = 1u << lane;
+        else hi = 1u << (lane - 32);
+    }
+    int anc = bad ? -1 : p;
+#pragma unroll
+    for (int s = 0; s < 6; ++s) {
+        const int src = anc >= 0 ? anc : lane;
+        const uint32_t lo_up = __shfl(lo, src);
+        const uint32_t hi_up = __shfl(hi, src);
+        const int bad_up = __shfl(bad, src);
+        const int anc_up = __shfl(anc, src);
+        if (anc >= 0) {
+            lo |= lo_up;
+            hi |= hi_up;
+            bad |= bad_up;
+            anc = anc_up;
+        }
+    }
+    if (!node) return;
+    const uint64_t m = bad ? 0ull : (((uint64_t)hi << 32) | lo);
+    mask[b * N + lane] = m;
+    depth[b * N + lane] = bad ? 0 : __popcll(m);
+}
+
+
+// ---- attention ----------------------------------------------------------------
+constexpr int kRowThreads = 256, kRowWaves = kRowThreads / kWave, kMaxD = 256;
+
+// The rows of sequence b: first row and count (clamped into [0, T)).
+__device__ __forceinline__ void rows_of(const int32_t* cu, int T, int B, int b, int* first, int* n) {
+    if (!cu) {
+        *n = T / B;
+        *first = b * *n;
+        return;
+    }
+    const int lo = min(max(cu[b], 0), T), hi = min(max(cu[b + 1], lo), T);
+    *first = lo;
+    *n = hi - lo;
+}
+
+// Which sequence row t belongs to: the last b with cu[b] <= t (-1: none).
+__device__ __forceinline__ int seq_of(const int32_t* cu, int T, int B, int t) {
+    if (!cu) return t / (T / B);
+    int lo = 0, hi = B;                       // cu[lo] <= t < cu[hi], if anywhere
+    if (t < cu[0] || t >= cu[B]) return -1;
+    while (hi - lo > 1) {
+        const int m = (lo + hi) / 2;
+        if (cu[m] <= t) lo = m;
+        else hi = m;
+    }
+    return lo;
+}
+
+// One wave per (row, query head): lanes over 64 keys for the scores, over D for the sums.
+template <bool PAGED>
+__global__ __launch_bounds__(kRowThreads) void attention_row_kernel(PagedArgs a, PromptArgs r) {
+    __shared__ float qs[kRowWaves][kMaxD];
+    const int w = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int T = PAGED ? a.T : r.T, Hq = PAGED ? a.Hq : r.Hq, H = PAGED ? a.H : r.H, D = PAGED ? a.D : r.D;
+    const int64_t item = (int64_t)blockIdx.x * kRowWaves + w;
+    const int t = (int)(item / Hq), head = (int)(item % Hq), kvh = head / (Hq / H);
+    const bool row = t < T;
+    const int b = row ? (PAGED ? seq_of(a.cu_q, T, a.B, t) : seq_of(r.cu, T, r.B, t)) : -1;
+    const uint16_t* q = (PAGED ? a.q + (int64_t)t * a.ld_q : r.q + (int64_t)t * r.ld_q) + (int64_t)head * D;
+    if (b >= 0)
+        for (int d = lane; d < D; d += kWave) qs[w][d] = bf16_to_f32(q[d]);
+    __syncthreads();
+    if (b < 0) return;
+    int first, n, L;
+    rows_of(PAGED ? a.cu_q : r.cu, T, PAGED ? a.B : r.B, b, &first, &n);
+    L = PAGED ? min(max(a.kv_lens[b], 0), a.max_len) : n;
+    const int i = t - first, last = PAGED && a.tree ? L - 1 : L - n + i;
+    const uint64_t mask = PAGED && a.tree && i > 0 ? a.tree[(int64_t)b * a.N + i - 1] : 0;
+    float m = -INFINITY, sum = 0.0f, o[kMaxD / kWave] = {};
+    for (int j0 = 0; j0 <= last; j0 += kWave) {
+        const int j = j0 + lane;
+        bool seen = j <= last;
+        int64_t at = 0;
+        if constexpr (PAGED) {
+            if (a.tree && seen && j >= L - a.N) seen = (mask >> (j - (L - a.N))) & 1;
+            int page = -1;
+            if (seen) page = a.tables[(int64_t)b * a.ld_tables + j / a.block_size];
+            seen = seen && page >= 0 && page < a.num_blocks;
+            at = seen ? ((int64_t)page * a.block_size + j % a.block_size) * H + kvh : 0;
+        } else {
+            at = (int64_t)(first + (seen ? j : 0));
+        }
+        float s = 0.0f, sv = 1.0f;
+        if (seen) {
+            for (int d = 0; d < D; d += 8) {
+                if constexpr (PAGED) {
+                    const uint2 c = *reinterpret_cast<const uint2*>(a.k_cache + at * D + d);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const uint32_t x = (e < 4 ? c.x : c.y) >> (8 * (e & 3));
+                        s = fmaf(qs[w][d + e], __builtin_amdgcn_cvt_f32_fp8((int)x, 0), s);
+                    }
+                } else {
+                    float k[8];
+                    unpack8(*reinterpret_cast<const uint4*>(r.k + at * r.ld_k + (int64_t)kvh * D + d), k);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s = fmaf(qs[w][d + e], k[e], s);
+                }
+            }
+            if constexpr (PAGED) {
+                s *= a.per_tensor ? a.k_scale[0] : a.k_scale[at];
+                sv = a.per_tensor ? a.v_scale[0] : a.v_scale[at];
+            }
+            s *= (PAGED ? a.scale : r.scale) * 1.44269504f;
+        } else {
+            s = -INFINITY;
+        }
+        const float top = fmaxf(m, wave_max(s));
+        const float ref = top == -INFINITY ? 0.0f : top;
+        const float down = exp2f(m - ref), p = exp2f(s - ref);
+        sum = sum * down + wave_sum(p);
+#pragma unroll
+        for (int x = 0; x < kMaxD / kWave; ++x) o[x] *= down;
+        m = top;
+        const uint64_t any = __ballot(seen);
+        const float pv = p * sv;
+        for (int u = 0; u < kWave; ++u) {
+            if (!((any >> u) & 1)) continue;
+            const float pu = __shfl(pv, u);
+            const int64_t au = __shfl(at, u);
+#pragma unroll
+            for (int x = 0; x < kMaxD / kWave; ++x) {
+                const int d = lane + kWave * x;
+                if (d < D) {
+                    float v;
+                    if constexpr (PAGED) v = __builtin_amdgcn_cvt_f32_fp8(a.v_cache[au * D + d], 0);
+                    else v = bf16_to_f32(r.v[au * r.ld_v + (int64_t)kvh * D + d]);
+                    o[x] = fmaf(pu, v, o[x]);
+                }
+            }
+        }
+    }
+    uint16_t* out = (PAGED ? a.out + (int64_t)t * a.ld_out : r.out + (int64_t)t * r.ld_out) + (int64_t)head * D;
+#pragma unroll
+    for (int x = 0; x < kMaxD / kWave; ++x) {
+        const int d = lane + kWave * x;
+        if (d < D) out[d] = (uint16_t)f32_to_bf16x2(sum != 0.0f ? o[x] / sum : 0.0f, 0.0f);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_paged_attention(const PagedArgs& a, void* workspace, hipStream_t stream) {
+    (void)workspace;
+    const int64_t items = (int64_t)a.T * a.Hq;
+    hipLaunchKernelGGL(attention_row_kernel<true>, dim3((unsigned)((items + kRowWaves - 1) / kRowWaves)),
+                       dim3(kRowThreads), 0, stream, a, PromptArgs{});
+    return hipGetLastError();
+}
+
+hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t stream) {
+    const int64_t items = (int64_t)a.T * a.Hq;
+    hipLaunchKernelGGL(attention_row_kernel<false>, dim3((unsigned)((items + kRowWaves - 1) / kRowWaves)),
+                       dim3(kRowThreads), 0, stream, PagedArgs{}, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_tree_mask(const int32_t* parents, int64_t B, int64_t N, uint64_t* mask, int32_t* depth,
+                            hipStream_t stream) {
+    const int64_t blocks = (B + kTmSeqPerBlock - 1) / kTmSeqPerBlock;
+    hipLaunchKernelGGL(tree_mask_kernel, dim3((unsigned)blocks), dim3(kTmThreads), 0, stream, parents, B, (int)N,
+                       mask, depth);
+    return hipGetLastError();
+}
+
+}  // namespace specfp8

@@ -5,6 +5,10 @@
 #include <stddef.h>
 #include <stdint.h>
 
+// Launchers that the host side of the ABI also links without (its checks run
+// in a library without device code); a call that reaches a missing one fails.
+#define SPEC_DEVICE_SIDE __attribute__((weak))
+
 namespace specfp8 {
 
 // ---- quantize.hip
@@ -24,6 +28,13 @@ hipError_t launch_kv_cache_write(const uint16_t* k, int64_t ld_k, const uint16_t
                                  const int64_t* slot_mapping, int64_t T, int64_t H, int64_t D,
                                  int64_t num_slots, int per_tensor, float* k_scale, float* v_scale,
                                  uint8_t* k_cache, uint8_t* v_cache, hipStream_t stream);
+
+// Codes of T tokens' cache rows back as bf16 ([T][ld], H heads of D values each);
+// tokens outside the cache read as zeros.
+SPEC_DEVICE_SIDE hipError_t launch_kv_cache_read(const uint8_t* k_cache, const uint8_t* v_cache, const float* k_scale,
+                                                 const float* v_scale, int per_tensor, const int64_t* slot_mapping,
+                                                 int64_t T, int64_t H, int64_t D, int64_t num_slots, uint16_t* k,
+                                                 int64_t ld_k, uint16_t* v, int64_t ld_v, hipStream_t stream);
 
 // ---- gemm.hip
 struct GemmPlan {
@@ -97,7 +108,34 @@ hipError_t launch_accept_tree(const AcceptPlan& p, const uint16_t* zt, const int
                               int32_t* out_tokens, int32_t* accepted_nodes, int32_t* num_accepted, void* workspace,
                               hipStream_t stream);
 
-// ---- tree_mask.hip
+// ---- attention.hip
+// Attention of new rows over the paged FP8 cache, and over packed bf16 prompts
+// (include/spec_fp8.h states the arguments).
+struct PagedArgs {
+    const uint16_t* q;
+    const uint8_t *k_cache, *v_cache;
+    const float *k_scale, *v_scale;
+    const int32_t *tables, *kv_lens, *cu_q;
+    const uint64_t* tree;
+    uint16_t* out;
+    int64_t ld_q, ld_out, ld_tables;
+    int32_t T, B, N, Hq, H, D, block_size, num_blocks, max_len;   // max_len: tokens that a table row can name
+    int32_t per_tensor;
+    float scale;
+};
+size_t paged_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D);
+SPEC_DEVICE_SIDE hipError_t launch_paged_attention(const PagedArgs& a, void* workspace, hipStream_t stream);
+
+struct PromptArgs {
+    const uint16_t *q, *k, *v;
+    const int32_t* cu;
+    uint16_t* out;
+    int64_t ld_q, ld_k, ld_v, ld_out;
+    int32_t T, B, Hq, H, D;
+    float scale;
+};
+SPEC_DEVICE_SIDE hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t stream);
+
 // Ancestor-or-self masks (bit j = node j) and depths of B trees of N <= 64
 // nodes, parents int32 [B][N]; mask uint64 [B][N], depth int32 [B][N].
 hipError_t launch_tree_mask(const int32_t* parents, int64_t B, int64_t N, uint64_t* mask, int32_t* depth,

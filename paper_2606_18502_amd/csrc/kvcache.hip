@@ -74,7 +74,61 @@ __global__ __launch_bounds__(kKvThreads) void kv_cache_write_kernel(KvArgs a) {
     *reinterpret_cast<uint2*>(s.cache + (slot * a.H + h) * a.D + (int64_t)j * 8) = o;
 }
 
+// The reverse: one lane per 8 codes of a (token, head) row, decoded, scaled in
+// fp32 and rounded once to bf16 (one 8-byte load, one 16-byte store).
+struct KvReadSide {
+    uint16_t* x;
+    int64_t ld_x;
+    const float* scale;
+    const uint8_t* cache;
+};
+
+struct KvReadArgs {
+    KvReadSide side[2];
+    const int64_t* slot;
+    int64_t T, H, D, num_slots;
+    int per_tensor;
+};
+
+__global__ __launch_bounds__(kKvThreads) void kv_cache_read_kernel(KvReadArgs a) {
+    const KvReadSide s = blockIdx.y ? a.side[1] : a.side[0];
+    const int64_t per_row = a.D / 8, item = (int64_t)blockIdx.x * kKvThreads + threadIdx.x;
+    const int64_t row = item / per_row, j = item - row * per_row;
+    if (row >= a.T * a.H) return;
+    const int64_t t = row / a.H, h = row - t * a.H, slot = a.slot[t];
+    uint4 o = {0, 0, 0, 0};
+    if (slot >= 0 && slot < a.num_slots) {
+        const int64_t r = slot * a.H + h;
+        const float sc = s.scale[a.per_tensor ? 0 : r];
+        const uint2 c = *reinterpret_cast<const uint2*>(s.cache + r * a.D + j * 8);
+        o.x = f32_to_bf16x2(__builtin_amdgcn_cvt_f32_fp8(c.x, 0) * sc, __builtin_amdgcn_cvt_f32_fp8(c.x, 1) * sc);
+        o.y = f32_to_bf16x2(__builtin_amdgcn_cvt_f32_fp8(c.x, 2) * sc, __builtin_amdgcn_cvt_f32_fp8(c.x, 3) * sc);
+        o.z = f32_to_bf16x2(__builtin_amdgcn_cvt_f32_fp8(c.y, 0) * sc, __builtin_amdgcn_cvt_f32_fp8(c.y, 1) * sc);
+        o.w = f32_to_bf16x2(__builtin_amdgcn_cvt_f32_fp8(c.y, 2) * sc, __builtin_amdgcn_cvt_f32_fp8(c.y, 3) * sc);
+    }
+    *reinterpret_cast<uint4*>(s.x + t * s.ld_x + h * a.D + j * 8) = o;
+}
+
 }  // namespace
+
+hipError_t launch_kv_cache_read(const uint8_t* k_cache, const uint8_t* v_cache, const float* k_scale,
+                                const float* v_scale, int per_tensor, const int64_t* slot_mapping, int64_t T,
+                                int64_t H, int64_t D, int64_t num_slots, uint16_t* k, int64_t ld_k, uint16_t* v,
+                                int64_t ld_v, hipStream_t stream) {
+    KvReadArgs a;
+    a.side[0] = KvReadSide{k, ld_k, k_scale, k_cache};
+    a.side[1] = KvReadSide{v, ld_v, v_scale, v_cache};
+    a.slot = slot_mapping;
+    a.T = T;
+    a.H = H;
+    a.D = D;
+    a.num_slots = num_slots;
+    a.per_tensor = per_tensor;
+    const int64_t lanes = T * H * (D / 8);
+    hipLaunchKernelGGL(kv_cache_read_kernel, dim3((unsigned)((lanes + kKvThreads - 1) / kKvThreads), 2),
+                       dim3(kKvThreads), 0, stream, a);
+    return hipGetLastError();
+}
 
 int64_t kv_group_lanes(int64_t D) {
     int64_t g = 1;

@@ -186,4 +186,6 @@ AcceptPlan plan_accept(int64_t B, int64_t k, int64_t V) {
     return p;
 }
 
+size_t paged_attention_workspace_bytes(int64_t, int64_t, int64_t, int64_t, int64_t) { return kAttnTicketBytes; }
+
 }  // namespace specfp8

@@ -95,4 +95,7 @@ constexpr int64_t kAcceptSlice = (int64_t)64 * kAcceptVecs * 8;          // 4096
 constexpr int kAcceptPerThread = kAcceptVecs * 8;                        // 64 logits per thread (sampling)
 constexpr int64_t kAcceptChunk = (int64_t)kAcceptThreads * kAcceptPerThread;   // 16384 logits per sampling block
 
+// ---- paged attention ----------------------------------------------------------
+constexpr size_t kAttnTicketBytes = 16384;   // at the start of the workspace, zero between calls
+
 }  // namespace specfp8

@@ -9,6 +9,7 @@
 // Every function takes the wrapper's arguments positionally, in the order of
 // its Python signature.  Invalid arguments raise ValueError, a failed call the
 // SpecError class handed over by init().
+#include <c10/hip/HIPGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -17,6 +18,7 @@
 #include <ATen/ops/zeros.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <string>
 
@@ -302,6 +304,203 @@ SPEC_PY(py_kv_cache_write) {
                                              (uint8_t*)vc.data_ptr(), s);
           }));
     Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
+// Tokens of a cache call: [T, H, D] with heads packed side by side.
+struct Heads {
+    int64_t T, H, D, ld;
+};
+Heads heads(const Tensor& t, const char* name) {
+    if (t.dim() != 3) value_error("%s must be 3-D [T, heads, D]", name);
+    const int64_t T = t.size(0), H = t.size(1), D = t.size(2);
+    if ((D > 1 && t.stride(2) != 1) || (H > 1 && t.stride(1) != D))
+        value_error("%s must have unit stride over D and heads packed side by side", name);
+    return {T, H, D, T > 1 ? t.stride(0) : H * D};
+}
+
+void same_device(const Tensor& t, const Tensor& like, const char* name) {
+    if (t.device() != like.device()) value_error("%s must be on the device of the other tensors", name);
+}
+
+// The paged cache and its scales.
+struct Cache {
+    const Tensor &k, &v, &ks, &vs;
+    int64_t slots, H, D;
+    spec_scale_mode mode;
+};
+Cache cache(PyObject* kc, PyObject* vc, PyObject* ks, PyObject* vs, bool fixed) {
+    Cache c{dev(kc, ScalarType::Byte, "k_cache"), dev(vc, ScalarType::Byte, "v_cache"),
+            dev(ks, ScalarType::Float, "k_scale"), dev(vs, ScalarType::Float, "v_scale"),
+            0, 0, 0, fixed ? SPEC_SCALE_PER_TENSOR : SPEC_SCALE_PER_ROW};
+    need(c.k.dim() == 3 && c.v.sizes() == c.k.sizes() && c.k.is_contiguous() && c.v.is_contiguous(),
+         "k_cache and v_cache must be contiguous [num_slots, H, D]");
+    c.slots = c.k.size(0);
+    c.H = c.k.size(1);
+    c.D = c.k.size(2);
+    if (fixed) {
+        need(c.ks.numel() == 1 && c.vs.numel() == 1, "per-tensor scales hold one fp32 value each");
+    } else {
+        auto rows = [&](const Tensor& t) {
+            return t.dim() == 2 && t.size(0) == c.slots && t.size(1) == c.H && t.is_contiguous();
+        };
+        need(rows(c.ks) && rows(c.vs), "per-row scales must be contiguous fp32 [num_slots, H]");
+    }
+    same_device(c.v, c.k, "v_cache");
+    same_device(c.ks, c.k, "k_scale");
+    same_device(c.vs, c.k, "v_scale");
+    return c;
+}
+
+// The stream to launch on: the current one of the tensors' device, which is made current for the call.
+struct OnDevice {
+    c10::hip::HIPGuard guard;
+    explicit OnDevice(const Tensor& t) : guard(t.device().index()) {}
+};
+
+// kv_cache_read(k_cache, v_cache, slot_mapping, k_scale, v_scale, per_tensor, k, v)
+SPEC_PY(py_kv_cache_read) {
+    HANDLE_TH_ERRORS
+    args(n, 8);
+    const Cache c = cache(a[0], a[1], a[3], a[4], truth(a[5]));
+    const Tensor& slots = dev(a[2], ScalarType::Long, "slot_mapping");
+    need(slots.dim() == 1 && slots.is_contiguous(), "slot_mapping must be a contiguous int64 [T]");
+    same_device(slots, c.k, "slot_mapping");
+    const int64_t T = slots.size(0);
+    const OnDevice on(c.k);
+    Out out[2];
+    int64_t ld[2];
+    for (int i = 0; i < 2; ++i) {
+        const char* const name = i ? "v" : "k";
+        out[i] = out_arg(a[6 + i], ScalarType::BFloat16, name,
+                         [&] { return new_empty({T, c.H, c.D}, ScalarType::BFloat16, c.k); });
+        const Heads h = heads(out[i].t, name);
+        need(h.T == T && h.H == c.H && h.D == c.D, "k and v must be [T, H, D]");
+        same_device(out[i].t, c.k, name);
+        ld[i] = h.ld;
+    }
+    void* const s = stream();
+    check("spec_fp8_kv_cache_read", call([&] {
+              return spec_fp8_kv_cache_read((const uint8_t*)c.k.data_ptr(), (const uint8_t*)c.v.data_ptr(),
+                                            (const float*)c.ks.data_ptr(), (const float*)c.vs.data_ptr(), c.mode,
+                                            (const int64_t*)slots.data_ptr(), T, c.H, c.D, c.slots, out[0].t.data_ptr(),
+                                            ld[0], out[1].t.data_ptr(), ld[1], s);
+          }));
+    return pair(out[0], out[1]);
+    END_HANDLE_TH_ERRORS
+}
+
+// A contiguous int32 [count] (what the caller's message says)
+const int32_t* int_vector(PyObject* o, int64_t count, const Tensor& like, const char* name, const char* message) {
+    const Tensor& t = dev(o, ScalarType::Int, name);
+    need(t.dim() == 1 && t.size(0) == count && t.is_contiguous(), message);
+    same_device(t, like, name);
+    return (const int32_t*)t.data_ptr();
+}
+
+// The softmax scale: a number, or 1/sqrt(D)
+float softmax_scale(PyObject* o, int64_t D) {
+    return o == Py_None ? (float)(1.0 / std::sqrt((double)std::max<int64_t>(D, 1))) : number(o);
+}
+
+int64_t whole(PyObject* o) {
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw python_error();
+    return v;
+}
+
+// The output of an attention over q [T, Hq, D]
+Out attention_out(PyObject* o, const Tensor& q, const Heads& h, int64_t* ld) {
+    Out out = out_arg(o, ScalarType::BFloat16, "out",
+                      [&] { return new_empty({h.T, h.H, h.D}, ScalarType::BFloat16, q); });
+    const Heads w = heads(out.t, "out");
+    need(w.T == h.T && w.H == h.H && w.D == h.D, "out must be [T, Hq, D] like q");
+    same_device(out.t, q, "out");
+    *ld = w.ld;
+    return out;
+}
+
+// paged_attention(q, k_cache, v_cache, k_scale, v_scale, block_tables, kv_lens, block_size, cu_q, tree_mask, scale,
+//                 per_tensor, out, workspace)
+SPEC_PY(py_paged_attention) {
+    HANDLE_TH_ERRORS
+    args(n, 14);
+    const Tensor& q = dev(a[0], ScalarType::BFloat16, "q");
+    const Heads h = heads(q, "q");
+    const Cache c = cache(a[1], a[2], a[3], a[4], truth(a[11]));
+    need(c.D == h.D, "q and the caches must have the same head size");
+    same_device(c.k, q, "k_cache");
+    const Tensor& tables = dev(a[5], ScalarType::Int, "block_tables");
+    need(tables.dim() == 2 && (tables.size(1) <= 1 || tables.stride(1) == 1),
+         "block_tables must be int32 [B, P] with unit stride over P");
+    same_device(tables, q, "block_tables");
+    const int64_t B = tables.size(0), P = tables.size(1);
+    const int64_t ld_t = B > 1 ? tables.stride(0) : P;
+    const int32_t* const lens = int_vector(a[6], B, q, "kv_lens", "kv_lens must be a contiguous int32 [B]");
+    const int64_t block = whole(a[7]);
+    need(block > 0, "block_size must be positive");
+    const int32_t* const cu = a[8] == Py_None ? nullptr
+        : int_vector(a[8], B + 1, q, "cu_q", "cu_q must be a contiguous int32 [B + 1]");
+    const uint64_t* tree = nullptr;
+    int64_t N = 0;
+    if (a[9] != Py_None) {
+        const Tensor& m = dev(a[9], ScalarType::Long, "tree_mask");
+        need(m.dim() == 2 && m.size(0) == B && m.size(1) >= 1 && m.is_contiguous(),
+             "tree_mask must be a contiguous int64 [B, N]");
+        same_device(m, q, "tree_mask");
+        need(!cu, "with tree_mask every sequence has N + 1 rows: cu_q must be None");
+        tree = (const uint64_t*)m.data_ptr();
+        N = m.size(1);
+        need(h.T == B * (N + 1), "with tree_mask [B, N] q must hold B * (N + 1) rows");
+    }
+    const float scale = softmax_scale(a[10], h.D);
+    const OnDevice on(q);
+    int64_t ld_out = 0;
+    Out out = attention_out(a[12], q, h, &ld_out);
+    const size_t bytes = spec_fp8_paged_attention_workspace_bytes(h.T, B, h.H, c.H, h.D);
+    Tensor ws;
+    if (a[13] != Py_None) {
+        const Tensor& w = any_tensor(a[13], "workspace");
+        if ((size_t)bytes_of(w) >= bytes) ws = w;
+    }
+    if (!ws.defined()) ws = at::zeros({(int64_t)std::max<size_t>(bytes, 1)}, q.options().dtype(ScalarType::Byte));
+    void* const s = stream();
+    check("spec_fp8_paged_attention", call([&] {
+              return spec_fp8_paged_attention(
+                  q.data_ptr(), h.ld, (const uint8_t*)c.k.data_ptr(), (const uint8_t*)c.v.data_ptr(),
+                  (const float*)c.ks.data_ptr(), (const float*)c.vs.data_ptr(), c.mode,
+                  (const int32_t*)tables.data_ptr(), ld_t, P, lens, cu, tree, N, h.T, B, h.H, c.H, h.D, block,
+                  c.slots / block, scale, out.t.data_ptr(), ld_out, ws.data_ptr(), (size_t)bytes_of(ws), s);
+          }));
+    return out.release();
+    END_HANDLE_TH_ERRORS
+}
+
+// prompt_attention(q, k, v, cu_seqlens, scale, out)
+SPEC_PY(py_prompt_attention) {
+    HANDLE_TH_ERRORS
+    args(n, 6);
+    const Tensor& q = dev(a[0], ScalarType::BFloat16, "q");
+    const Tensor& k = dev(a[1], ScalarType::BFloat16, "k");
+    const Tensor& v = dev(a[2], ScalarType::BFloat16, "v");
+    const Heads h = heads(q, "q"), hk = heads(k, "k"), hv = heads(v, "v");
+    need(hk.T == h.T && hk.D == h.D && v.sizes() == k.sizes(), "k and v must be [T, H, D] with q's T and D");
+    same_device(k, q, "k");
+    same_device(v, q, "v");
+    const Tensor& cu = dev(a[3], ScalarType::Int, "cu_seqlens");
+    need(cu.dim() == 1 && cu.size(0) >= 1 && cu.is_contiguous(), "cu_seqlens must be a contiguous int32 [B + 1]");
+    same_device(cu, q, "cu_seqlens");
+    const float scale = softmax_scale(a[4], h.D);
+    const OnDevice on(q);
+    int64_t ld_out = 0;
+    Out out = attention_out(a[5], q, h, &ld_out);
+    void* const s = stream();
+    check("spec_prompt_attention_bf16", call([&] {
+              return spec_prompt_attention_bf16(q.data_ptr(), h.ld, k.data_ptr(), hk.ld, v.data_ptr(), hv.ld,
+                                                (const int32_t*)cu.data_ptr(), h.T, cu.size(0) - 1, h.H, hk.H, h.D, scale,
+                                                out.t.data_ptr(), ld_out, s);
+          }));
+    return out.release();
     END_HANDLE_TH_ERRORS
 }
 
@@ -603,6 +802,9 @@ PyMethodDef g_methods[] = {
     SPEC_METHOD(silu_mul),
     SPEC_METHOD(clip_count),
     SPEC_METHOD(kv_cache_write),
+    SPEC_METHOD(kv_cache_read),
+    SPEC_METHOD(paged_attention),
+    SPEC_METHOD(prompt_attention),
     SPEC_METHOD(gemm),
     SPEC_METHOD(gemm_silu_mul),
     SPEC_METHOD(gemm_logit_stats),

@@ -67,6 +67,78 @@ spec_status check_kv_cache_write(const void* k, int64_t ld_k, const void* v, int
     return SPEC_OK;
 }
 
+spec_status check_kv_cache_read(const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                                int mode, const int64_t* slot_mapping, int64_t T, int64_t H, int64_t D,
+                                int64_t num_slots, const void* k, int64_t ld_k, const void* v, int64_t ld_v) {
+    // the write's rules; an empty cache has no rows to point at
+    const bool empty = num_slots == 0;
+    static const float unused = 0.0f;
+    return check_kv_cache_write(k, ld_k, v, ld_v, slot_mapping, T, H, D, num_slots, mode,
+                                empty && !k_scale ? &unused : k_scale, empty && !v_scale ? &unused : v_scale,
+                                empty ? k : k_cache, empty ? v : v_cache);
+}
+
+namespace {
+
+// Head counts, head size and scale that both attentions take.
+spec_status check_heads(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D, float scale) {
+    if (T < 0 || B < 0 || Hq <= 0 || H <= 0 || D <= 0 || Hq % H != 0) return SPEC_ERR_SHAPE;
+    if (D % 8 != 0 || D > 256) return SPEC_ERR_UNSUPPORTED;
+    if (Hq > kMaxGridY || T > kMaxGrid / Hq || B > kMaxGrid) return SPEC_ERR_UNSUPPORTED;
+    if (!isfinite(scale) || !(scale > 0.0f)) return SPEC_ERR_VALUE;
+    return SPEC_OK;
+}
+
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+}  // namespace
+
+spec_status check_paged_attention(const void* q, int64_t ld_q, const void* k_cache, const void* v_cache,
+                                  const float* k_scale, const float* v_scale, int mode, const int32_t* block_tables,
+                                  int64_t ld_tables, int64_t max_blocks, const int32_t* kv_lens, const int32_t* cu_q,
+                                  const uint64_t* tree_mask, int64_t N, int64_t T, int64_t B, int64_t Hq, int64_t H,
+                                  int64_t D, int64_t block_size, int64_t num_blocks, float scale, const void* out,
+                                  int64_t ld_out) {
+    if (mode != SPEC_SCALE_PER_ROW && mode != SPEC_SCALE_PER_TENSOR) return SPEC_ERR_ENUM;
+    const spec_status st = check_heads(T, B, Hq, H, D, scale);
+    if (st != SPEC_OK) return st;
+    if (block_size <= 0 || num_blocks < 0 || max_blocks < 0 || ld_tables < max_blocks) return SPEC_ERR_SHAPE;
+    if (num_blocks > kMaxGrid || block_size > kMaxGrid || max_blocks > kMaxGrid / block_size)
+        return SPEC_ERR_UNSUPPORTED;
+    if (num_blocks > INT64_MAX / (block_size * H) / D || (B > 0 && ld_tables > INT64_MAX / 4 / B))
+        return SPEC_ERR_UNSUPPORTED;
+    if (ld_q < Hq * D || ld_out < Hq * D) return SPEC_ERR_SHAPE;
+    if ((tree_mask == nullptr) != (N == 0)) return SPEC_ERR_SHAPE;
+    if (tree_mask) {
+        if (N < 0 || cu_q || T != B * (N + 1)) return SPEC_ERR_SHAPE;
+        if (N > 64) return SPEC_ERR_UNSUPPORTED;
+    }
+    if (T == 0 || B == 0) return SPEC_OK;
+    if (!cu_q && T % B != 0) return SPEC_ERR_SHAPE;
+    if (!q || !out || !kv_lens || (max_blocks > 0 && !block_tables)) return SPEC_ERR_NULL;
+    if (num_blocks > 0 && (!k_cache || !v_cache || !k_scale || !v_scale)) return SPEC_ERR_NULL;
+    if (ld_q % 8 != 0 || ld_out % 8 != 0 || !aligned16(q) || !aligned16(out)) return SPEC_ERR_ALIGN;
+    if (!aligned16(k_cache) || !aligned16(v_cache)) return SPEC_ERR_ALIGN;
+    if (!aligned4(k_scale) || !aligned4(v_scale) || !aligned4(block_tables) || !aligned4(kv_lens) || !aligned4(cu_q))
+        return SPEC_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(tree_mask) & 7u) != 0) return SPEC_ERR_ALIGN;
+    return SPEC_OK;
+}
+
+spec_status check_prompt_attention(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v,
+                                   int64_t ld_v, const int32_t* cu_seqlens, int64_t T, int64_t B, int64_t Hq,
+                                   int64_t H, int64_t D, float scale, const void* out, int64_t ld_out) {
+    const spec_status st = check_heads(T, B, Hq, H, D, scale);
+    if (st != SPEC_OK) return st;
+    if (ld_q < Hq * D || ld_out < Hq * D || ld_k < H * D || ld_v < H * D) return SPEC_ERR_SHAPE;
+    if (T == 0 || B == 0) return SPEC_OK;
+    if (!q || !k || !v || !out || !cu_seqlens) return SPEC_ERR_NULL;
+    if (ld_q % 8 != 0 || ld_k % 8 != 0 || ld_v % 8 != 0 || ld_out % 8 != 0) return SPEC_ERR_ALIGN;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned4(cu_seqlens))
+        return SPEC_ERR_ALIGN;
+    return SPEC_OK;
+}
+
 spec_status check_tree_mask(const int32_t* parents, int64_t B, int64_t N, const uint64_t* mask,
                             const int32_t* depth) {
     if (B < 0 || N < 1) return SPEC_ERR_SHAPE;

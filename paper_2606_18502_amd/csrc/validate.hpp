@@ -23,6 +23,18 @@ spec_status check_kv_cache_write(const void* k, int64_t ld_k, const void* v, int
                                  const int64_t* slot_mapping, int64_t T, int64_t H, int64_t D, int64_t num_slots,
                                  int mode, const float* k_scale, const float* v_scale, const void* k_cache,
                                  const void* v_cache);
+spec_status check_kv_cache_read(const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                                int mode, const int64_t* slot_mapping, int64_t T, int64_t H, int64_t D,
+                                int64_t num_slots, const void* k, int64_t ld_k, const void* v, int64_t ld_v);
+spec_status check_paged_attention(const void* q, int64_t ld_q, const void* k_cache, const void* v_cache,
+                                  const float* k_scale, const float* v_scale, int mode, const int32_t* block_tables,
+                                  int64_t ld_tables, int64_t max_blocks, const int32_t* kv_lens, const int32_t* cu_q,
+                                  const uint64_t* tree_mask, int64_t N, int64_t T, int64_t B, int64_t Hq, int64_t H,
+                                  int64_t D, int64_t block_size, int64_t num_blocks, float scale, const void* out,
+                                  int64_t ld_out);
+spec_status check_prompt_attention(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v,
+                                   int64_t ld_v, const int32_t* cu_seqlens, int64_t T, int64_t B, int64_t Hq,
+                                   int64_t H, int64_t D, float scale, const void* out, int64_t ld_out);
 spec_status check_logit_stats(int64_t M, int64_t V, float temperature, const void* logits, int64_t ld_logits,
                               const float* stats, int64_t ld_stats, int64_t n_groups);
 spec_status check_accept_stats(const float* target_stats, int64_t n_stats, int64_t ld_stats, int64_t B);

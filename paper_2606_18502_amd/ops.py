@@ -76,6 +76,60 @@ def kv_cache_write(k: torch.Tensor, v: torch.Tensor, slot_mapping: torch.Tensor,
     (_bind or _load_bind()).kv_cache_write(k, v, slot_mapping, k_cache, v_cache, k_scale, v_scale, per_tensor)
 
 
+def kv_cache_read(k_cache: torch.Tensor, v_cache: torch.Tensor, slot_mapping: torch.Tensor, k_scale: torch.Tensor,
+                  v_scale: torch.Tensor, per_tensor: bool = False, k: Optional[torch.Tensor] = None,
+                  v: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Rows of the FP8 KV cache back as bf16 (spec_fp8_kv_cache_read).
+
+    Caches, scales and slot_mapping as for kv_cache_write; a slot outside the
+    cache reads as zeros.  k, v: bf16 [T, H, D] outputs (views as kv_cache_write
+    takes them; new ones if None).  Returns (k, v).
+    """
+    return (_bind or _load_bind()).kv_cache_read(k_cache, v_cache, slot_mapping, k_scale, v_scale, per_tensor, k, v)
+
+
+def paged_attention_workspace_bytes(T: int, B: int, Hq: int, H: int, D: int) -> int:
+    return int(_lib.load().spec_fp8_paged_attention_workspace_bytes(T, B, Hq, H, D))
+
+
+def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: torch.Tensor,
+                    v_scale: torch.Tensor, block_tables: torch.Tensor, kv_lens: torch.Tensor, block_size: int,
+                    cu_q: Optional[torch.Tensor] = None, tree_mask: Optional[torch.Tensor] = None,
+                    scale: Optional[float] = None, per_tensor: bool = False, out: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of new tokens over the paged FP8 KV cache (spec_fp8_paged_attention).
+
+    q: bf16 [T, Hq, D] view (heads packed side by side, e.g. the query columns
+    of the QKV output); k_cache, v_cache uint8 [num_slots, H, D] and their
+    scales as kv_cache_write leaves them, the new tokens included;
+    block_tables: int32 [B, P] (page of every block_size tokens); kv_lens: int32
+    [B], cached tokens of each sequence, the new ones last.  Rows: T/B for each
+    sequence, or cu_q int32 [B+1]; with tree_mask (int64 [B, N] of
+    tree_attention_mask) N+1 each: the root's and the nodes'.  scale: 1/sqrt(D)
+    if None.  Returns out bf16 [T, Hq, D]; given with cu_q, rows outside
+    [cu_q[0], cu_q[B]) stay as they were (a new one holds anything there).
+    workspace: paged_attention_workspace_bytes(T, B, Hq, H, D) bytes on the GPU, 16-byte
+    aligned, zero-filled once and then kept for all calls of a stream.  Bring
+    one: without it (or with one too small) every call zero-fills a new one.
+    """
+    return (_bind or _load_bind()).paged_attention(q, k_cache, v_cache, k_scale, v_scale, block_tables, kv_lens,
+                                                   block_size, cu_q, tree_mask, scale, per_tensor, out, workspace)
+
+
+def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor,
+                     scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Causal attention over packed prompts (spec_prompt_attention_bf16).
+
+    q: bf16 [T, Hq, D]; k, v: bf16 [T, H, D] (views with heads packed side by
+    side, e.g. the column blocks of the QKV output); cu_seqlens: int32 [B+1],
+    first row of every prompt and the end of the last.  scale: 1/sqrt(D) if
+    None.  Returns out bf16 [T, Hq, D]; rows outside [cu_seqlens[0],
+    cu_seqlens[B]) of a given one stay as they were (a new one holds anything
+    there).
+    """
+    return (_bind or _load_bind()).prompt_attention(q, k, v, cu_seqlens, scale, out)
+
+
 def gemm_workspace_bytes(M: int, N: int, K: int) -> int:
     return int(_lib.load().spec_fp8_gemm_workspace_bytes(M, N, K))
 
