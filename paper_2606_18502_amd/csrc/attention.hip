@@ -8,8 +8,10 @@
 // so six steps of lane exchanges (no memory traffic) cover any depth up to
 // 64.  A node whose parent is not one of the earlier nodes (or -1) poisons
 // itself and, through the same exchanges, every node below it.
-#include "device_common.hpp"
-#include "kernels.hpp"
+#include <algorithm>
+
+#include "attn_common.hpp"
+#include "attn_stream.hpp"
 
 namespace specfp8 {
 
@@ -56,18 +58,6 @@ __global__ __launch_bounds__(kTmThreads) void tree_mask_kernel(const int32_t* __
 
 // ---- attention ----------------------------------------------------------------
 constexpr int kRowThreads = 256, kRowWaves = kRowThreads / kWave, kMaxD = 256;
-
-// The rows of sequence b: first row and count (clamped into [0, T)).
-__device__ __forceinline__ void rows_of(const int32_t* cu, int T, int B, int b, int* first, int* n) {
-    if (!cu) {
-        *n = T / B;
-        *first = b * *n;
-        return;
-    }
-    const int lo = min(max(cu[b], 0), T), hi = min(max(cu[b + 1], lo), T);
-    *first = lo;
-    *n = hi - lo;
-}
 
 // Which sequence row t belongs to: the last b with cu[b] <= t (-1: none).
 __device__ __forceinline__ int seq_of(const int32_t* cu, int T, int B, int t) {
@@ -176,8 +166,43 @@ __global__ __launch_bounds__(kRowThreads) void attention_row_kernel(PagedArgs a,
 
 }  // namespace
 
-hipError_t launch_paged_attention(const PagedArgs& a, void* workspace, hipStream_t stream) {
-    (void)workspace;
+namespace {
+
+template <int DP, int NQ, int HG>
+hipError_t launch_stream(const PagedArgs& a, void* workspace, hipStream_t stream) {
+    using C = StreamShape<DP, NQ, HG, 2, 4>;
+    // The lengths are the device's: never more workgroups than there are steps where every sequence fills its table,
+    // at two steps each (fewer are not worth a join).
+    const int64_t units = ((int64_t)a.T * (a.Hq / a.H) / C::kRows + a.B) * ((a.H + HG - 1) / HG);
+    const int64_t steps = units * std::max<int64_t>((a.max_len + C::kStep - 1) / C::kStep, 1);
+    const int grid = (int)std::max<int64_t>(std::min<int64_t>(steps / 2, kAttnGroups), 1);
+    float* const part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace) + kAttnTicketBytes);
+    hipLaunchKernelGGL((paged_stream_kernel<DP, NQ, HG, 2, 4>), dim3(grid), dim3(256), C::kLds, stream, a, part,
+                       reinterpret_cast<unsigned int*>(workspace), grid, 2, C::KW == 1 ? 5 : 3);
+    return hipGetLastError();
+}
+
+template <int DP>
+hipError_t launch_stream_rows(const PagedPlan& p, const PagedArgs& a, void* workspace, hipStream_t stream) {
+    if (p.hg == 1)
+        return p.nq == 1 ? launch_stream<DP, 1, 1>(a, workspace, stream) : launch_stream<DP, 2, 1>(a, workspace, stream);
+    if (p.hg == 2)
+        return p.nq == 1 ? launch_stream<DP, 1, 2>(a, workspace, stream) : launch_stream<DP, 2, 2>(a, workspace, stream);
+    return launch_stream<DP, 1, 4>(a, workspace, stream);
+}
+
+}  // namespace
+
+hipError_t launch_paged_attention(const PagedArgs& given, void* workspace, hipStream_t stream) {
+    PagedArgs a = given;
+    if (a.num_blocks == 0) {             // no cache: every page is outside it, and loads need some address (q's first row)
+        a.k_cache = a.v_cache = reinterpret_cast<const uint8_t*>(a.q);
+        a.k_scale = a.v_scale = reinterpret_cast<const float*>(a.q);
+    }
+    const PagedPlan p = plan_paged(a.T, a.B, a.Hq, a.H, a.D);
+    if (p.dp == 64) return launch_stream_rows<64>(p, a, workspace, stream);
+    if (p.dp == 128) return launch_stream_rows<128>(p, a, workspace, stream);
+    if (p.dp == 256) return launch_stream_rows<256>(p, a, workspace, stream);
     const int64_t items = (int64_t)a.T * a.Hq;
     hipLaunchKernelGGL(attention_row_kernel<true>, dim3((unsigned)((items + kRowWaves - 1) / kRowWaves)),
                        dim3(kRowThreads), 0, stream, a, PromptArgs{});

@@ -1,0 +1,676 @@
+// Attention of few rows over the paged FP8 cache (single tokens, drafted
+// chains, trees): a stream over the cache.
+//
+// Mathematics.  With t_j = s_ij log2(e), a running reference m and
+// p_j = 2^(t_j - m):  out = sum_j p_j v_j / sum_j p_j.  The reference moves only when a
+// score exceeds it by more than 2^8 (kLazy): p then stays below 2^8, sums and
+// products are fp32, and nearly every tile skips the rescale and the lane
+// exchange that a maximum per tile needs.
+//
+// Work.  A unit is (sequence, 16*NQ rows, HG KV heads); its cost is its number of
+// key steps.  The steps of all units lie on one line, and the workgroups cut
+// it into equal ranges, whatever the sequences' lengths, which only the device
+// knows.  A range covers whole units and parts of at most two; the parts of a unit are
+// joined by the workgroup that stores the last of them (a ticket per unit, at
+// the workgroup where the unit starts).
+//
+// A wave owns one KV head and every KW-th tile of 32 keys, for all rows of the unit:
+// no data is shared between waves, so nothing waits at a barrier until the
+// end of a unit.  Codes go from HBM to LDS without registers (16 bytes per
+// lane from its key's page) into a ring of S stages; table entries of the tile
+// after next travel the same way.
+//   S^T = K Q^T  on v_mfma_f32_16x16x32_bf16: codes are exact in bf16.  A lane holds
+//     the scores of one row (lane % 16) at keys 4 (lane/16) + 0..3 and 16 more.
+//   O^T = V^T P^T: the 8 probabilities of a lane are, as they are, the 8 k-slots of
+//     its operand when V^T is read with keys in the same order, which the
+//     transposing LDS read (ds_read_b64_tr_b8, 8 keys of one channel per lane) does.
+// Chunks of a row lie at slot c ^ f(key) so that the 16 lanes that an LDS cycle
+// serves hit different banks.
+#pragma once
+
+#include <type_traits>
+
+#include "attn_common.hpp"
+
+namespace specfp8 {
+
+namespace {
+
+constexpr int kJoin = 16;                                    // parts that one workgroup joins at a time
+
+// LDS slot of 16-byte chunk c of key row r (0..31): c ^ this.  K: lanes l and l+16 (l % 16 < 8) are
+// served together, rows 0..7 at chunks 2x and 2x+1.  V: lanes 0..31, 16 rows (0..7
+// and 16..23, or 8..15 and 24..31) at one chunk.  Rows of DP bytes: 256/DP of
+// them share one line of banks.
+template <int DP>
+__device__ __forceinline__ int k_swizzle(int r) {
+    if constexpr (DP == 64) return 2 * ((r >> 2) & 1);
+    else if constexpr (DP == 128) return 2 * ((r >> 1) & 3);
+    else return 2 * (r & 7);
+}
+template <int DP>
+__device__ __forceinline__ int v_swizzle(int r) {
+    if constexpr (DP == 64) return ((r >> 2) & 1) | (((r >> 4) & 1) << 1);
+    else if constexpr (DP == 128) return ((r >> 1) & 3) | (((r >> 4) & 1) << 2);
+    else return (r & 7) | (((r >> 4) & 1) << 3);
+}
+
+template <int DP, int NQ, int HG, int S, int W>
+struct StreamShape {
+    static constexpr int KW = W / HG;             // waves that share a head
+    static constexpr int kRows = 16 * NQ;
+    static constexpr int kStep = 32 * KW;                    // keys of a step
+    static constexpr int kTile = 32 * DP;                    // bytes of a tile's K (V) codes
+    static constexpr int kStage = 2 * kTile + 256;           // and 64 scales
+    static constexpr int kTables = S * kStage;               // two tiles' table entries
+    static constexpr int kOffs = kTables + S * 256;          // byte offsets of a tile's rows
+    static constexpr int kWave = (kOffs + 256 + DP - 1) / DP * DP;
+    static constexpr int kLds = W * kWave;
+    static constexpr int kData = DP / 16 + 1;                // loads of a stage
+    static constexpr int kBlocks = DP / 16;
+    static constexpr int kPart = kRows * (DP + 4);           // floats of a head's part: sums, and four of each row
+    static_assert(S >= 2 && S <= 4 && (S - 2) * (kData + 1) < 64, "the waits below count these");
+    static_assert(kStage % DP == 0 && kWave % DP == 0, "a V row's address has no bits where its chunks' are");
+    static_assert(KW == 1 || W / 2 * NQ * (kBlocks * 256 + 128) * 4 <= kLds, "half the waves' results fit for the join");
+};
+
+template <int DP, int NQ, int HG, int S, int W>
+__global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel(PagedArgs a, float* part, unsigned int* tickets,
+                                                                      int groups, int min_steps, int extra) {
+    using C = StreamShape<DP, NQ, HG, S, W>;
+    constexpr int kStreamThreads = 64 * W, kStreamWaves = W;
+    constexpr int NB = C::kBlocks, KS = DP / 64;
+    // (sized at the launch: with the size in its view the compiler counts on one workgroup per CU, and then keeps the
+    // sums in AGPRs and copies them for every rescale)
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+    __shared__ int64_t scan[kStreamWaves + 1];
+    __shared__ int64_t found[2];
+    __shared__ int is_last;
+    __shared__ int window[3][32];                            // first row, rows and tokens of some sequences
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int G = a.Hq / a.H, NHG = (a.H + HG - 1) / HG;
+    const int q16 = lane & 15, qd = lane >> 4;
+
+    // ---- this workgroup's range of the line of steps
+    const auto steps_of = [&](int b, int* n, int* first, int* L, int* tiles) -> int {
+        rows_of(a.cu_q, a.T, a.B, b, first, n);
+        *L = min(max(a.kv_lens[b], 0), a.max_len);
+        *tiles = (int)(((int64_t)*n * G + C::kRows - 1) / C::kRows);
+        return max((*L + C::kStep - 1) / C::kStep, 1);
+    };
+    const int per = (a.B + kStreamThreads - 1) / kStreamThreads;
+    int64_t mine = 0;
+    for (int x = 0; x < per; ++x) {
+        const int b = tid * per + x;
+        if (b >= a.B) break;
+        int n, first, L, tiles;
+        const int st = steps_of(b, &n, &first, &L, &tiles);
+        mine += (int64_t)tiles * NHG * (st + extra);
+    }
+    int64_t upto = mine;
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t v = __shfl_up(upto, o);
+        if (lane >= o) upto += v;
+    }
+    if (lane == 63) scan[w] = upto;
+    __syncthreads();
+    int64_t total = 0, before = 0;
+    for (int x = 0; x < kStreamWaves; ++x) {
+        if (x < w) before += scan[x];
+        total += scan[x];
+    }
+    total = uniform(total);
+    before += upto - mine;
+    // never more workgroups than steps (in twos and so on: min_steps), so that every one has a step
+    const int64_t wanted = total / min_steps;
+    const int ng = uniform((int)(wanted < 1 ? 1 : (wanted < groups ? wanted : groups)));
+    if (total == 0 || (int)blockIdx.x >= ng) return;
+    // workgroups go round-robin over the XCDs: neighbours on the line share an XCD's L2
+    const int xcd = blockIdx.x % 8, at = blockIdx.x / 8;
+    const int wg = xcd * (ng / 8) + min(xcd, ng % 8) + at;
+    const int64_t lo = uniform(total * wg / ng), hi = uniform(total * (wg + 1) / ng);
+    if (lo >= before && lo < before + mine) {
+        int64_t base = before;
+        for (int x = 0; x < per; ++x) {
+            const int b = tid * per + x;
+            int n, first, L, tiles;
+            const int st = steps_of(b, &n, &first, &L, &tiles);
+            const int64_t cost = (int64_t)tiles * NHG * (st + extra);
+            if (lo < base + cost) {
+                found[0] = b;
+                found[1] = base;
+                break;
+            }
+            base += cost;
+        }
+    }
+    __syncthreads();
+    int b = uniform((int)found[0]);
+    int64_t base = uniform(found[1]);
+
+    // ---- this wave's corner of LDS
+    const int hw = w % HG, kw = w / HG;
+    uint8_t* const ring = smem + w * C::kWave;
+    const uint32_t ring_at = __builtin_amdgcn_readfirstlane(lds_at(ring));
+    const uint32_t* const tab = reinterpret_cast<const uint32_t*>(ring + C::kTables);
+    int64_t* const offs = reinterpret_cast<int64_t*>(ring + C::kOffs);
+    // loads of K and V: lane -> key row and chunk of the 1 KiB of a load
+    constexpr int kKeys = 1024 / DP;                         // keys of a load
+    const int ld_key = lane / (DP / 16), ld_slot = lane % (DP / 16);
+    const int chunks = a.D / 16;
+    const int bs = a.block_size, step_q = C::kStep / bs, step_r = C::kStep % bs;
+    const int last_block = max(a.max_len / bs - 1, 0);
+    const float* const scales = lane < 32 ? a.k_scale : a.v_scale;
+    const uint64_t page_rows = (uint64_t)bs * (uint32_t)a.H;
+    const float c2 = a.scale * 1.4426950408889634f;
+
+    int64_t pos = lo;
+    int window_at = b - 32;
+    while (pos < hi) {
+        if (b >= window_at + 32) {
+            window_at = b;
+            __syncthreads();
+            if (tid < 32 && b + tid < a.B) {
+                int n, first;
+                rows_of(a.cu_q, a.T, a.B, b + tid, &first, &n);
+                window[0][tid] = first;
+                window[1][tid] = n;
+                window[2][tid] = min(max(a.kv_lens[b + tid], 0), a.max_len);
+            }
+            __syncthreads();
+        }
+        const int first = uniform(window[0][b - window_at]), n = uniform(window[1][b - window_at]);
+        const int L = uniform(window[2][b - window_at]);
+        const int tiles = (int)(((int64_t)n * G + C::kRows - 1) / C::kRows);
+        const int st = max((L + C::kStep - 1) / C::kStep, 1);
+        const int64_t cost = (int64_t)tiles * NHG * (st + extra);
+        if (pos >= base + cost) {
+            base += cost;
+            ++b;
+            continue;
+        }
+        // a unit's stretch of the line: `extra` for its beginning, then its steps
+        const int64_t rel = pos - base;
+        const int unit = uniform((int)(rel / (st + extra)));
+        const int64_t u0 = base + (int64_t)unit * (st + extra) + extra;               // where its steps lie
+        const int s_in = (int)max(pos - u0, (int64_t)0), s_out = (int)min(hi - u0, (int64_t)st);
+        pos = u0 + max(s_out, 0);
+        if (s_out <= s_in) break;                       // its beginning alone lies in this range
+        const int rt = unit / NHG, hg = unit % NHG;
+        const int count = s_out - s_in;
+        const int R = n * G, head = hg * HG + hw;
+        const bool active = head < a.H;
+
+        f32x4_t o[NQ][NB];
+        float m[NQ], l[NQ];
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) {
+            m[x] = kLowest;
+            l[x] = 0.0f;
+#pragma unroll
+            for (int d = 0; d < NB; ++d) o[x][d] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        if (active) {
+            // ---- the rows: queries, and what each sees
+            bf16x8_t q[NQ][KS][2];
+            int lim[NQ];
+            std::conditional_t<(NB > 8), uint64_t, uint32_t> marked[NQ];          // channels of this lane that a NaN code reached
+            uint64_t tree[NQ];
+#pragma unroll
+            for (int x = 0; x < NQ; ++x) {
+                const int row = rt * C::kRows + x * 16 + q16, i = row / G, g = row - i * G;
+                const bool there = row < R;
+                const uint16_t* src = a.q + (int64_t)(first + (there ? i : 0)) * a.ld_q + (int64_t)(head * G + (there ? g : 0)) * a.D;
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const int d = 64 * s + 16 * qd + 8 * u;
+                        // (a row that is not there reads the first; a channel past the head's end becomes 0)
+                        u32x4_t v = *reinterpret_cast<const u32x4_t*>(src + min(d, a.D - 8));
+                        if (d >= a.D) v = u32x4_t{0, 0, 0, 0};
+                        q[x][s][u] = __builtin_bit_cast(bf16x8_t, v);
+                    }
+                marked[x] = 0;
+                lim[x] = there ? L - n + i : -1;
+                tree[x] = a.tree && there && i > 0 ? a.tree[(int64_t)b * a.N + i - 1] : 0;
+                if (a.tree) lim[x] = there ? L - 1 : -1;
+            }
+            const int all_see = a.tree ? L - a.N - 1 : L - n + rt * C::kRows / G;   // tokens up to here are seen by every row
+
+            // ---- the ring
+            const int32_t* const table = a.max_len > 0 ? a.tables + (int64_t)b * a.ld_tables : a.kv_lens;
+            const int key = lane & 31;
+            const int first_key = 32 * (s_in * C::KW + kw);
+            int blk = (first_key + key) / bs, off_t = (first_key + key) - blk * bs, off_p = off_t;
+            const auto load_table = [&](int t) {
+                load_lds4(table + min(blk, last_block), ring_at + C::kTables + (t % S) * 256);
+                off_t += step_r;
+                blk += step_q;
+                if (off_t >= bs) {
+                    off_t -= bs;
+                    ++blk;
+                }
+            };
+            int next_key = first_key;
+            const auto prepare = [&](int t) -> uint32_t {            // byte offsets and scales of tile t; which keys there are
+                const int page = (int)tab[(t % S) * 64 + lane];
+                const bool there = next_key + key < L && page >= 0 && page < a.num_blocks;
+                const uint32_t pg = there ? page : 0, of = there ? off_p : 0;
+                const uint64_t row = pg * page_rows + (of * (uint64_t)(uint32_t)a.H + (uint32_t)head);
+                if (lane < 32) offs[key] = (int64_t)(row * (uint32_t)a.D);
+                load_lds4(scales + (a.per_tensor ? 0 : row), ring_at + (t % S) * C::kStage + 2 * C::kTile);
+                off_p += step_r;
+                if (off_p >= bs) off_p -= bs;
+                next_key += C::kStep;
+                return (uint32_t)__ballot(there);
+            };
+            const auto load_codes = [&](int t) {
+                const uint32_t to = ring_at + (t % S) * C::kStage;
+#pragma unroll
+                for (int x = 0; x < C::kTile / 1024; ++x) {
+                    const int r = x * kKeys + ld_key;
+                    const int64_t at_row = offs[r];
+                    const int ck = ld_slot ^ k_swizzle<DP>(r), cv = ld_slot ^ v_swizzle<DP>(r);
+                    // (chunks past the head's end: the row's first one; their queries are 0)
+                    load_lds16(a.k_cache + at_row + (ck < chunks ? ck * 16 : 0), to + x * 1024);
+                    load_lds16(a.v_cache + at_row + (cv < chunks ? cv * 16 : 0), to + C::kTile + x * 1024);
+                }
+            };
+            // A tile's group of loads: its scales, the table entries of the tile S - 1 later, its codes.  In order, so
+            // that a tile's codes are there when its group's count is, and the table entries that the next group
+            // needs with them.
+            uint32_t th[S];
+            const auto load_group = [&](int t) -> uint32_t {
+                const uint32_t there = prepare(t);
+                if (t + S - 1 < count) load_table(t + S - 1);
+                load_codes(t);
+                return there;
+            };
+            wait_lds();
+#pragma unroll
+            for (int t = 0; t < S - 1; ++t)
+                if (t < count) load_table(t);
+            wait_loads<0>();
+            // (the queries, too: a wait for them in the loop would drain the ring)
+#pragma unroll
+            for (int x = 0; x < NQ; ++x)
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) asm volatile("" : "+v"(q[x][s][u]));
+#pragma unroll
+            for (int t = 0; t < S - 1; ++t) {
+                th[t] = 0;
+                if (t < count) th[t] = load_group(t);
+            }
+
+            // One tile; full: every row sees every key of it.
+            const auto attend = [&](int t, int k0, uint32_t there, bool full) {
+                const uint32_t stage = ring_at + (t % S) * C::kStage;
+                const uint8_t* const kt = ring + (t % S) * C::kStage;
+                const float* const sc = reinterpret_cast<const float*>(kt + 2 * C::kTile);
+
+                // ---- scores
+                f32x4_t s[2][NQ];
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+                    for (int x = 0; x < NQ; ++x) s[kb][x] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int u = 0; u < KS; ++u) {
+                        const int r = kb * 16 + q16;
+                        const u32x4_t c = *reinterpret_cast<const u32x4_t*>(
+                            kt + r * DP + (((4 * u + qd) ^ k_swizzle<DP>(r)) << 4));
+                        const bf16x8_t lo8 = codes_to_bf16(c[0], c[1]), hi8 = codes_to_bf16(c[2], c[3]);
+#pragma unroll
+                        for (int x = 0; x < NQ; ++x) {
+                            s[kb][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo8, q[x][u][0], s[kb][x], 0, 0, 0);
+                            s[kb][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi8, q[x][u][1], s[kb][x], 0, 0, 0);
+                        }
+                    }
+                }
+                // values, read ahead of their use: lane j of 16 addresses half j % 2 of key row 16 (j/8) + 4 qd + (j/2) % 4
+                const int vr = 16 * (q16 >> 3) + 4 * qd + ((q16 >> 1) & 3);
+                const uint32_t vat = stage + C::kTile + vr * DP + (v_swizzle<DP>(vr) << 4) + 8 * (q16 & 1);
+                const auto values_at = [&](int d) {
+                    return __builtin_amdgcn_ds_read_tr8_b64_v2i32((SPEC_LDS i32x2_t*)(uintptr_t)(vat ^ (d << 4)));
+                };
+                i32x2_t vc[NB];
+#pragma unroll
+                for (int d = 0; d < NB; ++d) vc[d] = values_at(d);
+                const f32x4_t sk0 = *reinterpret_cast<const f32x4_t*>(sc + 4 * qd) * c2;
+                const f32x4_t sk1 = *reinterpret_cast<const f32x4_t*>(sc + 16 + 4 * qd) * c2;
+                const f32x4_t sv0 = *reinterpret_cast<const f32x4_t*>(sc + 32 + 4 * qd);
+                const f32x4_t sv1 = *reinterpret_cast<const f32x4_t*>(sc + 48 + 4 * qd);
+                uint32_t seen[NQ];
+                float top[NQ];
+                bool over = false;
+#pragma unroll
+                for (int x = 0; x < NQ; ++x) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        s[0][x][r] *= sk0[r];
+                        s[1][x][r] *= sk1[r];
+                    }
+                    if (!full) {
+                        uint32_t see = 0;
+                        const int d = lim[x] - k0;
+                        if (d >= 0) see = d >= 31 ? 0xffffffffu : (2u << d) - 1u;
+                        if (a.tree) {
+                            const int f = k0 - (L - a.N);                         // node number of the tile's first key
+                            if (f >= 0) see &= f < 64 ? (uint32_t)(tree[x] >> f) : 0u;
+                            else if (f > -32) see &= (uint32_t)(tree[x] << -f) | ((1u << -f) - 1u);
+                        }
+                        see &= there;
+                        seen[x] = see >> (4 * qd);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            s[0][x][r] = (seen[x] >> r) & 1 ? s[0][x][r] : -INFINITY;
+                            s[1][x][r] = (seen[x] >> (16 + r)) & 1 ? s[1][x][r] : -INFINITY;
+                        }
+                    }
+                    float t0 = fmaxf(fmaxf(s[0][x][0], s[0][x][1]), fmaxf(s[0][x][2], s[0][x][3]));
+                    float t1 = fmaxf(fmaxf(s[1][x][0], s[1][x][1]), fmaxf(s[1][x][2], s[1][x][3]));
+                    top[x] = fmaxf(t0, t1);
+                    over = over || top[x] > m[x] + kLazy;
+                }
+                if (__ballot(over)) {
+#pragma unroll
+                    for (int x = 0; x < NQ; ++x) {
+                        const float mx = fmaxf(m[x], max_quarters(top[x]));
+                        const float down = exp2_hw(m[x] - mx);
+                        m[x] = mx;
+                        l[x] *= down;
+#pragma unroll
+                        for (int d = 0; d < NB; ++d) o[x][d] *= down;
+                    }
+                }
+                // ---- probabilities, as the second product's operand
+                bf16x8_t pv[NQ];
+#pragma unroll
+                for (int x = 0; x < NQ; ++x) {
+                    float p0[4], p1[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        p0[r] = exp2_hw(s[0][x][r] - m[x]);
+                        p1[r] = exp2_hw(s[1][x][r] - m[x]);
+                    }
+                    l[x] += ((p0[0] + p0[1]) + (p0[2] + p0[3])) + ((p1[0] + p1[1]) + (p1[2] + p1[3]));
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        p0[r] *= sv0[r];
+                        p1[r] *= sv1[r];
+                        if (!full) {                     // an infinite or NaN scale of a key not seen
+                            p0[r] = (seen[x] >> r) & 1 ? p0[r] : 0.0f;
+                            p1[r] = (seen[x] >> (16 + r)) & 1 ? p1[r] : 0.0f;
+                        }
+                    }
+                    u32x4_t v;
+                    v[0] = f32_to_bf16x2(p0[0], p0[1]);
+                    v[1] = f32_to_bf16x2(p0[2], p0[3]);
+                    v[2] = f32_to_bf16x2(p1[0], p1[1]);
+                    v[3] = f32_to_bf16x2(p1[2], p1[3]);
+                    pv[x] = __builtin_bit_cast(bf16x8_t, v);
+                }
+                // ---- sums of values
+                if (!full) {
+                    // Keys that are not there: code 0.  A NaN code reaches the rows that see its key and no others
+                    // (0 * NaN is NaN): it counts 0 in the sums, and its rows are marked.
+                    const uint32_t keep0 = ((((there >> (4 * qd)) & 15u) * 0x00204081u) & 0x01010101u) * 0xffu;
+                    const uint32_t keep1 = ((((there >> (16 + 4 * qd)) & 15u) * 0x00204081u) & 0x01010101u) * 0xffu;
+                    uint32_t nans = 0;
+#pragma unroll
+                    for (int d = 0; d < NB; ++d) {
+                        const uint32_t c0 = (uint32_t)vc[d][0] & keep0, c1 = (uint32_t)vc[d][1] & keep1;
+                        const uint32_t n0 = nan_bytes(c0) >> 7, n1 = nan_bytes(c1) >> 7;
+                        nans |= n0 | n1;
+                        vc[d][0] = (int)(c0 & ~(n0 * 0xffu));
+                        vc[d][1] = (int)(c1 & ~(n1 * 0xffu));
+                    }
+                    if (__ballot(nans != 0)) {
+                        // (keys that hold one) x (keys that a row sees), as a product of ones
+#pragma unroll 1
+                        for (int d = 0; d < NB; ++d) {
+                            const i32x2_t c = values_at(d);
+                            const uint32_t n0 = nan_bytes((uint32_t)c[0] & keep0) >> 7;
+                            const uint32_t n1 = nan_bytes((uint32_t)c[1] & keep1) >> 7;
+                            u32x4_t has;
+                            has[0] = ones((n0 & 1u) | ((n0 >> 7) & 2u));
+                            has[1] = ones(((n0 >> 16) & 1u) | ((n0 >> 23) & 2u));
+                            has[2] = ones((n1 & 1u) | ((n1 >> 7) & 2u));
+                            has[3] = ones(((n1 >> 16) & 1u) | ((n1 >> 23) & 2u));
+#pragma unroll
+                            for (int x = 0; x < NQ; ++x) {
+                                u32x4_t sees;
+#pragma unroll
+                                for (int y = 0; y < 4; ++y) sees[y] = ones(seen[x] >> ((y >> 1) * 16 + (y & 1) * 2));
+                                const f32x4_t hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                    __builtin_bit_cast(bf16x8_t, has), __builtin_bit_cast(bf16x8_t, sees),
+                                    f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+#pragma unroll
+                                for (int r = 0; r < 4; ++r)
+                                    marked[x] |= (decltype(marked[x] + 0))(hits[r] > 0.0f ? 1 : 0) << (4 * d + r);
+                            }
+                        }
+                    }
+                }
+#pragma unroll
+                for (int d = 0; d < NB; ++d) {
+                    const bf16x8_t vt = codes_to_bf16((uint32_t)vc[d][0], (uint32_t)vc[d][1]);
+#pragma unroll
+                    for (int x = 0; x < NQ; ++x)
+                        o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pv[x], o[x][d], 0, 0, 0);
+                }
+            };
+
+            for (int t = 0; t < count; ++t) {
+                // codes of t: the groups behind it are those of t+1 .. t+S-2
+                const int behind = min(S - 2, count - 1 - t);
+                if (t + 2 * S - 3 < count) wait_loads<(S - 2) * (C::kData + 1)>();
+                else if (S > 3 && behind == 2) wait_loads<(S > 3 ? 2 : 0) * C::kData>();
+                else if (S > 2 && behind >= 1) wait_loads<(S > 2 ? 1 : 0) * C::kData>();
+                else wait_loads<0>();
+                wait_lds();
+                th[S - 1] = 0;
+                if (t + S - 1 < count) th[S - 1] = load_group(t + S - 1);
+                const int k0 = first_key + t * C::kStep;
+                attend(t, k0, th[0], th[0] == 0xffffffffu && k0 + 31 <= all_see);
+#pragma unroll
+                for (int x = 0; x + 1 < S; ++x) th[x] = th[x + 1];
+            }
+#pragma unroll
+            for (int x = 0; x < NQ; ++x) {
+                l[x] = sum_quarters(l[x]);
+                if (__ballot(marked[x] != 0)) {
+#pragma unroll
+                    for (int d = 0; d < NB; ++d)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if ((marked[x] >> (4 * d + r)) & 1) o[x][d][r] = __builtin_nanf("");
+                }
+            }
+        }
+
+        // ---- waves that share a head join through LDS (odd ones into even ones, then 2 into 0)
+        if constexpr (C::KW > 1) {
+            float* const box = reinterpret_cast<float*>(smem);
+#pragma unroll
+            for (int gap = 1; gap < C::KW; gap *= 2) {
+                __syncthreads();
+                const bool gives = (kw & (2 * gap - 1)) == gap, takes = (kw & (2 * gap - 1)) == 0;
+                float* const to = box + ((kw / (2 * gap)) * HG + hw) * (NQ * (NB * 256 + 128));
+                if (gives) {
+#pragma unroll
+                    for (int x = 0; x < NQ; ++x) {
+#pragma unroll
+                        for (int d = 0; d < NB; ++d)
+                            *reinterpret_cast<f32x4_t*>(to + x * (NB * 256 + 128) + d * 256 + lane * 4) = o[x][d];
+                        to[x * (NB * 256 + 128) + NB * 256 + lane] = m[x];
+                        to[x * (NB * 256 + 128) + NB * 256 + 64 + lane] = l[x];
+                    }
+                }
+                __syncthreads();
+                if (takes) {
+#pragma unroll
+                    for (int x = 0; x < NQ; ++x) {
+                        const float mo = to[x * (NB * 256 + 128) + NB * 256 + lane];
+                        const float lo2 = to[x * (NB * 256 + 128) + NB * 256 + 64 + lane];
+                        const float mx = fmaxf(m[x], mo), da = exp2_hw(m[x] - mx), db = exp2_hw(mo - mx);
+                        m[x] = mx;
+                        l[x] = l[x] * da + lo2 * db;
+#pragma unroll
+                        for (int d = 0; d < NB; ++d) {
+                            const f32x4_t v =
+                                *reinterpret_cast<const f32x4_t*>(to + x * (NB * 256 + 128) + d * 256 + lane * 4);
+                            o[x][d] = o[x][d] * da + v * db;
+                        }
+                    }
+                }
+            }
+            __syncthreads();
+        }
+
+        const auto store_rows = [&](int x, int h, float total_l, const f32x4_t (&v)[NB]) {
+            const int row = rt * C::kRows + x * 16 + q16, i = row / G, g = row - i * G;
+            if (row >= R) return;
+            const float inv = total_l == 0.0f ? 0.0f : 1.0f / total_l;
+            uint16_t* const dst = a.out + (int64_t)(first + i) * a.ld_out + (int64_t)(h * G + g) * a.D + 4 * qd;
+#pragma unroll
+            for (int d = 0; d < NB; ++d) {
+                if (16 * d < a.D) {
+                    uint2 y;
+                    y.x = f32_to_bf16x2(v[d][0] * inv, v[d][1] * inv);
+                    y.y = f32_to_bf16x2(v[d][2] * inv, v[d][3] * inv);
+                    *reinterpret_cast<uint2*>(dst + 16 * d) = y;
+                }
+            }
+        };
+
+        if (count == st) {
+            if (active && kw == 0) {
+#pragma unroll
+                for (int x = 0; x < NQ; ++x) store_rows(x, head, l[x], o[x]);
+            }
+        } else {
+            // ---- A part of a unit: to the workspace.  The last to arrive joins the parts in the line's order; many
+            // parts in two rounds, the first over runs of parts whose result takes the place of the run's first.
+            const int64_t u1 = u0 + st - 1;               // (its last step)
+            const int w0 = uniform((int)(((u0 + 1) * ng - 1) / total)), w1 = uniform((int)(((u1 + 1) * ng - 1) / total));
+            const int parts = w1 - w0 + 1, run = parts <= 3 * kJoin / 2 ? parts : kJoin;
+            const int runs = (parts + run - 1) / run, r0 = (wg - w0) / run * run;
+            const auto slot_of = [&](int x) { return 2 * (w0 + x) + (x == 0 ? 1 : 0); };      // of the unit's part x
+            // a part: HG heads of kRows rows of DP sums, then their references and sums of p, and those of a run
+            const auto part_of = [&](int x) { return part + (int64_t)slot_of(x) * (HG * C::kPart); };
+            const auto ml_of = [&](int x, int round) {
+                return reinterpret_cast<uint64_t*>(part_of(x) + HG * C::kRows * DP) + round * HG * C::kRows;
+            };
+            if (active && kw == 0) {
+                float* const to = part_of(wg - w0) + hw * C::kRows * DP;
+#pragma unroll
+                for (int x = 0; x < NQ; ++x) {
+                    if (rt * C::kRows + x * 16 + q16 < R) {
+#pragma unroll
+                        for (int d = 0; d < NB; ++d)
+                            if (16 * d < a.D) store_agent(to + (x * 16 + q16) * DP + 16 * d + 4 * qd, o[x][d]);
+                        if (qd == 0)
+                            __hip_atomic_store(ml_of(wg - w0, 0) + hw * C::kRows + x * 16 + q16, two_floats(m[x], l[x]),
+                                               __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    }
+                }
+            }
+            // true in the workgroup that is the last of `expected`; what the others stored is there then
+            const auto last_of = [&](unsigned int* ticket, int expected) {
+                wait_loads<0>();                         // this wave's stores are acknowledged
+                __syncthreads();
+                if (tid == 0) {
+                    is_last = (int)__hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+                              expected - 1;
+                    if (is_last) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                }
+                __syncthreads();
+                return is_last != 0;
+            };
+            // Parts x0, x0 + step, .. below x1, in the line's order whoever came last, to the output or to the place of
+            // the first.  A thread takes four channels of K rows; 8 parts of them are in flight at a time.
+            const auto join = [&](int x0, int x1, int step, int round, bool output) {
+                constexpr int K = 2, Z = 8;
+                const int zs = (x1 - x0 + step - 1) / step, quads = a.D / 4;
+                const int Rt = min(R - rt * C::kRows, C::kRows), all = min(a.H - hg * HG, HG) * Rt * quads;
+                for (int e0 = 0; e0 < all; e0 += K * kStreamThreads) {
+                    int from[K], at_row[K];
+                    f32x4_t acc[K];
+                    float mx[K], sum[K];
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        const int e = min(e0 + k * kStreamThreads + tid, all - 1), y = e / quads;
+                        at_row[k] = y / Rt * C::kRows + y % Rt;
+                        from[k] = at_row[k] * DP + (e - y * quads) * 4;
+                        acc[k] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+                        mx[k] = kLowest;
+                        sum[k] = 0.0f;
+                    }
+                    for (int z0 = 0; z0 < zs; z0 += Z) {
+                        f32x4_t v[Z][K];
+                        uint64_t ml[Z][K];
+#pragma unroll
+                        for (int u = 0; u < Z; ++u)
+#pragma unroll
+                            for (int k = 0; k < K; ++k) {
+                                const int x = x0 + min(z0 + u, zs - 1) * step;
+                                ml[u][k] = __hip_atomic_load(ml_of(x, round) + at_row[k], __ATOMIC_RELAXED,
+                                                             __HIP_MEMORY_SCOPE_AGENT);
+                                v[u][k] = load_agent(part_of(x) + from[k]);
+                            }
+#pragma unroll
+                        for (int k = 0; k < K; ++k) {
+                            float top = mx[k];
+#pragma unroll
+                            for (int u = 0; u < Z; ++u) top = fmaxf(top, __uint_as_float((uint32_t)ml[u][k]));
+                            const float down = exp2_hw(mx[k] - top);
+                            mx[k] = top;
+                            sum[k] *= down;
+                            acc[k] *= down;
+#pragma unroll
+                            for (int u = 0; u < Z; ++u)
+                                if (z0 + u < zs) {
+                                    const float f = exp2_hw(__uint_as_float((uint32_t)ml[u][k]) - top);
+                                    sum[k] += __uint_as_float((uint32_t)(ml[u][k] >> 32)) * f;
+                                    acc[k] += v[u][k] * f;
+                                }
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        if (e0 + k * kStreamThreads + tid >= all) break;
+                        const int d = from[k] - at_row[k] * DP;
+                        if (output) {
+                            const int h = at_row[k] / C::kRows, row = rt * C::kRows + at_row[k] % C::kRows;
+                            const int i = row / G, g = row - i * G;
+                            const float f = sum[k] == 0.0f ? 0.0f : 1.0f / sum[k];
+                            uint2 y;
+                            y.x = f32_to_bf16x2(acc[k][0] * f, acc[k][1] * f);
+                            y.y = f32_to_bf16x2(acc[k][2] * f, acc[k][3] * f);
+                            *reinterpret_cast<uint2*>(a.out + (int64_t)(first + i) * a.ld_out +
+                                                      (int64_t)((hg * HG + h) * G + g) * a.D + d) = y;
+                        } else {
+                            store_agent(part_of(x0) + from[k], acc[k]);
+                            if (d == 0)
+                                __hip_atomic_store(ml_of(x0, 1) + at_row[k], two_floats(mx[k], sum[k]), __ATOMIC_RELAXED,
+                                                   __HIP_MEMORY_SCOPE_AGENT);
+                        }
+                    }
+                }
+            };
+            if (last_of(tickets + slot_of(r0), min(run, parts - r0))) {
+                join(r0, min(r0 + run, parts), 1, 0, runs == 1);
+                if (runs > 1 && last_of(tickets + 2 * groups + w0, runs)) join(0, parts, run, 1, true);
+            }
+            __syncthreads();
+        }
+    }
+}
+
+}  // namespace
+
+}  // namespace specfp8

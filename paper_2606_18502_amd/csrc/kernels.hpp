@@ -123,7 +123,7 @@ struct PagedArgs {
     int32_t per_tensor;
     float scale;
 };
-size_t paged_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D);
+size_t paged_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D);   // plan.cpp
 SPEC_DEVICE_SIDE hipError_t launch_paged_attention(const PagedArgs& a, void* workspace, hipStream_t stream);
 
 struct PromptArgs {

@@ -186,6 +186,19 @@ AcceptPlan plan_accept(int64_t B, int64_t k, int64_t V) {
     return p;
 }
 
-size_t paged_attention_workspace_bytes(int64_t, int64_t, int64_t, int64_t, int64_t) { return kAttnTicketBytes; }
+PagedPlan plan_paged(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D) {
+    PagedPlan p{0, 1, 1, kAttnTicketBytes};
+    if (D % 16 != 0) return p;
+    p.dp = D <= 64 ? 64 : (D <= 128 ? 128 : 256);
+    const int64_t rows = (T + B - 1) / B * (Hq / H);       // of an average sequence and one KV head
+    p.nq = rows <= 16 ? 1 : 2;
+    p.hg = H == 1 ? 1 : (H == 2 || p.nq == 2 ? 2 : 4);
+    p.bytes += (size_t)kAttnGroups * 2 * p.hg * p.nq * 16 * (p.dp + 4) * sizeof(float);
+    return p;
+}
+
+size_t paged_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D) {
+    return plan_paged(T, B, Hq, H, D).bytes;
+}
 
 }  // namespace specfp8

@@ -97,5 +97,14 @@ constexpr int64_t kAcceptChunk = (int64_t)kAcceptThreads * kAcceptPerThread;   /
 
 // ---- paged attention ----------------------------------------------------------
 constexpr size_t kAttnTicketBytes = 16384;   // at the start of the workspace, zero between calls
+constexpr int kAttnGroups = 256;             // workgroups of a stream over the cache, one ticket each
+
+// A call's kernel: D padded to dp (64, 128, 256; 0: the row kernel, for heads that are no multiple
+// of 16), 16*nq rows per unit, hg KV heads per workgroup.
+struct PagedPlan {
+    int dp, nq, hg;
+    size_t bytes;          // of workspace: the tickets, then two parts per workgroup
+};
+PagedPlan plan_paged(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D);
 
 }  // namespace specfp8

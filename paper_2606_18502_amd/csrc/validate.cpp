@@ -11,6 +11,7 @@ inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 
 
 constexpr int64_t kMaxGrid = 2147483647;   // grid.x limit
 constexpr int64_t kMaxGridY = 65535;       // grid.y limit
+constexpr int64_t kMaxTokens = kMaxGrid - 65535;   // of a sequence: positions a few tiles further still fit
 
 }  // namespace
 
@@ -103,7 +104,7 @@ spec_status check_paged_attention(const void* q, int64_t ld_q, const void* k_cac
     const spec_status st = check_heads(T, B, Hq, H, D, scale);
     if (st != SPEC_OK) return st;
     if (block_size <= 0 || num_blocks < 0 || max_blocks < 0 || ld_tables < max_blocks) return SPEC_ERR_SHAPE;
-    if (num_blocks > kMaxGrid || block_size > kMaxGrid || max_blocks > kMaxGrid / block_size)
+    if (num_blocks > kMaxGrid || block_size > kMaxTokens || max_blocks > kMaxTokens / block_size)
         return SPEC_ERR_UNSUPPORTED;
     if (num_blocks > INT64_MAX / (block_size * H) / D || (B > 0 && ld_tables > INT64_MAX / 4 / B))
         return SPEC_ERR_UNSUPPORTED;
