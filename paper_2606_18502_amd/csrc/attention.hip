@@ -12,6 +12,7 @@
 
 #include "attn_common.hpp"
 #include "attn_stream.hpp"
+#include "attn_tile.hpp"
 
 namespace specfp8 {
 
@@ -210,6 +211,15 @@ hipError_t launch_paged_attention(const PagedArgs& given, void* workspace, hipSt
 }
 
 hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t stream) {
+    const int64_t G = a.Hq / a.H, slots = (int64_t)a.T * G / 128 + a.B;
+    if (a.D <= 128 && slots * a.H * 256 <= 0xffffffffll) {
+        const dim3 grid((unsigned)(slots * a.H)), block(256);
+        if (a.D <= 64)
+            hipLaunchKernelGGL(prompt_tile_kernel<64>, grid, block, TileShape_<64>::kLds, stream, a, (int)slots);
+        else
+            hipLaunchKernelGGL(prompt_tile_kernel<128>, grid, block, TileShape_<128>::kLds, stream, a, (int)slots);
+        return hipGetLastError();
+    }
     const int64_t items = (int64_t)a.T * a.Hq;
     hipLaunchKernelGGL(attention_row_kernel<false>, dim3((unsigned)((items + kRowWaves - 1) / kRowWaves)),
                        dim3(kRowThreads), 0, stream, PagedArgs{}, a);
