@@ -7,13 +7,7 @@
 // products are fp32, and nearly every tile skips the rescale and the lane
 // exchange that a maximum per tile needs.
 //
-// Work.  A unit is (sequence, 16*NQ rows, HG KV heads); its cost is its number of
-// key steps.  The steps of all units lie on one line, and the workgroups cut
-// it into equal ranges, whatever the sequences' lengths, which only the device
-// knows.  A range covers whole units and parts of at most two; the parts of a unit are
-// joined by the workgroup that stores the last of them (a ticket per unit, at
-// the workgroup where the unit starts).
-//
+// Work: attn_line.hpp; a unit is (sequence, 16*NQ rows, HG KV heads).
 // A wave owns one KV head and every KW-th tile of 32 keys, for all rows of the unit:
 // no data is shared between waves, so nothing waits at a barrier until the
 // end of a unit.  Codes go from HBM to LDS without registers (16 bytes per
@@ -30,13 +24,12 @@
 
 #include <type_traits>
 
-#include "attn_common.hpp"
+#include "attn_line.hpp"
 
 namespace specfp8 {
 
 namespace {
 
-constexpr int kJoin = 16;                                    // parts that one workgroup joins at a time
 
 // LDS slot of 16-byte chunk c of key row r (0..31): c ^ this.  K: lanes l and l+16 (l % 16 < 8) are
 // served together, rows 0..7 at chunks 2x and 2x+1.  V: lanes 0..31, 16 rows (0..7
@@ -68,7 +61,6 @@ struct StreamShape {
     static constexpr int kLds = W * kWave;
     static constexpr int kData = DP / 16 + 1;                // loads of a stage
     static constexpr int kBlocks = DP / 16;
-    static constexpr int kPart = kRows * (DP + 4);           // floats of a head's part: sums, and four of each row
     static_assert(S >= 2 && S <= 4 && (S - 2) * (kData + 1) < 64, "the waits below count these");
     static_assert(kStage % DP == 0 && kWave % DP == 0, "a V row's address has no bits where its chunks' are");
     static_assert(KW == 1 || W / 2 * NQ * (kBlocks * 256 + 128) * 4 <= kLds, "half the waves' results fit for the join");
@@ -78,75 +70,17 @@ template <int DP, int NQ, int HG, int S, int W>
 __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel(PagedArgs a, float* part, unsigned int* tickets,
                                                                       int groups, int min_steps, int extra) {
     using C = StreamShape<DP, NQ, HG, S, W>;
-    constexpr int kStreamThreads = 64 * W, kStreamWaves = W;
     constexpr int NB = C::kBlocks, KS = DP / 64;
     // (sized at the launch: with the size in its view the compiler counts on one workgroup per CU, and then keeps the
     // sums in AGPRs and copies them for every rescale)
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
-    __shared__ int64_t scan[kStreamWaves + 1];
-    __shared__ int64_t found[2];
-    __shared__ int is_last;
-    __shared__ int window[3][32];                            // first row, rows and tokens of some sequences
+    __shared__ LineShared<64 * W> sh;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int G = a.Hq / a.H, NHG = (a.H + HG - 1) / HG;
     const int q16 = lane & 15, qd = lane >> 4;
 
-    // ---- this workgroup's range of the line of steps
-    const auto steps_of = [&](int b, int* n, int* first, int* L, int* tiles) -> int {
-        rows_of(a.cu_q, a.T, a.B, b, first, n);
-        *L = min(max(a.kv_lens[b], 0), a.max_len);
-        *tiles = (int)(((int64_t)*n * G + C::kRows - 1) / C::kRows);
-        return max((*L + C::kStep - 1) / C::kStep, 1);
-    };
-    const int per = (a.B + kStreamThreads - 1) / kStreamThreads;
-    int64_t mine = 0;
-    for (int x = 0; x < per; ++x) {
-        const int b = tid * per + x;
-        if (b >= a.B) break;
-        int n, first, L, tiles;
-        const int st = steps_of(b, &n, &first, &L, &tiles);
-        mine += (int64_t)tiles * NHG * (st + extra);
-    }
-    int64_t upto = mine;
-    for (int o = 1; o < 64; o <<= 1) {
-        const int64_t v = __shfl_up(upto, o);
-        if (lane >= o) upto += v;
-    }
-    if (lane == 63) scan[w] = upto;
-    __syncthreads();
-    int64_t total = 0, before = 0;
-    for (int x = 0; x < kStreamWaves; ++x) {
-        if (x < w) before += scan[x];
-        total += scan[x];
-    }
-    total = uniform(total);
-    before += upto - mine;
-    // never more workgroups than steps (in twos and so on: min_steps), so that every one has a step
-    const int64_t wanted = total / min_steps;
-    const int ng = uniform((int)(wanted < 1 ? 1 : (wanted < groups ? wanted : groups)));
-    if (total == 0 || (int)blockIdx.x >= ng) return;
-    // workgroups go round-robin over the XCDs: neighbours on the line share an XCD's L2
-    const int xcd = blockIdx.x % 8, at = blockIdx.x / 8;
-    const int wg = xcd * (ng / 8) + min(xcd, ng % 8) + at;
-    const int64_t lo = uniform(total * wg / ng), hi = uniform(total * (wg + 1) / ng);
-    if (lo >= before && lo < before + mine) {
-        int64_t base = before;
-        for (int x = 0; x < per; ++x) {
-            const int b = tid * per + x;
-            int n, first, L, tiles;
-            const int st = steps_of(b, &n, &first, &L, &tiles);
-            const int64_t cost = (int64_t)tiles * NHG * (st + extra);
-            if (lo < base + cost) {
-                found[0] = b;
-                found[1] = base;
-                break;
-            }
-            base += cost;
-        }
-    }
-    __syncthreads();
-    int b = uniform((int)found[0]);
-    int64_t base = uniform(found[1]);
+    Line<64 * W, C::kRows, C::kStep> line;
+    if (!line.begin(a, sh, HG, groups, min_steps, extra)) return;
 
     // ---- this wave's corner of LDS
     const int hw = w % HG, kw = w / HG;
@@ -164,40 +98,9 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
     const uint64_t page_rows = (uint64_t)bs * (uint32_t)a.H;
     const float c2 = a.scale * 1.4426950408889634f;
 
-    int64_t pos = lo;
-    int window_at = b - 32;
-    while (pos < hi) {
-        if (b >= window_at + 32) {
-            window_at = b;
-            __syncthreads();
-            if (tid < 32 && b + tid < a.B) {
-                int n, first;
-                rows_of(a.cu_q, a.T, a.B, b + tid, &first, &n);
-                window[0][tid] = first;
-                window[1][tid] = n;
-                window[2][tid] = min(max(a.kv_lens[b + tid], 0), a.max_len);
-            }
-            __syncthreads();
-        }
-        const int first = uniform(window[0][b - window_at]), n = uniform(window[1][b - window_at]);
-        const int L = uniform(window[2][b - window_at]);
-        const int tiles = (int)(((int64_t)n * G + C::kRows - 1) / C::kRows);
-        const int st = max((L + C::kStep - 1) / C::kStep, 1);
-        const int64_t cost = (int64_t)tiles * NHG * (st + extra);
-        if (pos >= base + cost) {
-            base += cost;
-            ++b;
-            continue;
-        }
-        // a unit's stretch of the line: `extra` for its beginning, then its steps
-        const int64_t rel = pos - base;
-        const int unit = uniform((int)(rel / (st + extra)));
-        const int64_t u0 = base + (int64_t)unit * (st + extra) + extra;               // where its steps lie
-        const int s_in = (int)max(pos - u0, (int64_t)0), s_out = (int)min(hi - u0, (int64_t)st);
-        pos = u0 + max(s_out, 0);
-        if (s_out <= s_in) break;                       // its beginning alone lies in this range
-        const int rt = unit / NHG, hg = unit % NHG;
-        const int count = s_out - s_in;
+    while (line.next(a, sh)) {
+        const int first = line.first, n = line.n, L = line.L, rt = line.rt, hg = line.hg, s_in = line.s_in, count = line.count;
+        const int b = line.b;
         const int R = n * G, head = hg * HG + hw;
         const bool active = head < a.H;
 
@@ -547,126 +450,26 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
             }
         };
 
-        if (count == st) {
+        if (line.whole()) {
             if (active && kw == 0) {
 #pragma unroll
                 for (int x = 0; x < NQ; ++x) store_rows(x, head, l[x], o[x]);
             }
         } else {
-            // ---- A part of a unit: to the workspace.  The last to arrive joins the parts in the line's order; many
-            // parts in two rounds, the first over runs of parts whose result takes the place of the run's first.
-            const int64_t u1 = u0 + st - 1;               // (its last step)
-            const int w0 = uniform((int)(((u0 + 1) * ng - 1) / total)), w1 = uniform((int)(((u1 + 1) * ng - 1) / total));
-            const int parts = w1 - w0 + 1, run = parts <= 3 * kJoin / 2 ? parts : kJoin;
-            const int runs = (parts + run - 1) / run, r0 = (wg - w0) / run * run;
-            const auto slot_of = [&](int x) { return 2 * (w0 + x) + (x == 0 ? 1 : 0); };      // of the unit's part x
-            // a part: HG heads of kRows rows of DP sums, then their references and sums of p, and those of a run
-            const auto part_of = [&](int x) { return part + (int64_t)slot_of(x) * (HG * C::kPart); };
-            const auto ml_of = [&](int x, int round) {
-                return reinterpret_cast<uint64_t*>(part_of(x) + HG * C::kRows * DP) + round * HG * C::kRows;
-            };
+            const Parts<64 * W, C::kRows, C::kStep, HG, DP> parts(line, part, tickets, groups);
             if (active && kw == 0) {
-                float* const to = part_of(wg - w0) + hw * C::kRows * DP;
+                float* const to = parts.sums(parts.me) + hw * C::kRows * DP;
 #pragma unroll
                 for (int x = 0; x < NQ; ++x) {
                     if (rt * C::kRows + x * 16 + q16 < R) {
 #pragma unroll
                         for (int d = 0; d < NB; ++d)
                             if (16 * d < a.D) store_agent(to + (x * 16 + q16) * DP + 16 * d + 4 * qd, o[x][d]);
-                        if (qd == 0)
-                            __hip_atomic_store(ml_of(wg - w0, 0) + hw * C::kRows + x * 16 + q16, two_floats(m[x], l[x]),
-                                               __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                        if (qd == 0) parts.store_ml(hw * C::kRows + x * 16 + q16, m[x], l[x]);
                     }
                 }
             }
-            // true in the workgroup that is the last of `expected`; what the others stored is there then
-            const auto last_of = [&](unsigned int* ticket, int expected) {
-                wait_loads<0>();                         // this wave's stores are acknowledged
-                __syncthreads();
-                if (tid == 0) {
-                    is_last = (int)__hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
-                              expected - 1;
-                    if (is_last) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                }
-                __syncthreads();
-                return is_last != 0;
-            };
-            // Parts x0, x0 + step, .. below x1, in the line's order whoever came last, to the output or to the place of
-            // the first.  A thread takes four channels of K rows; 8 parts of them are in flight at a time.
-            const auto join = [&](int x0, int x1, int step, int round, bool output) {
-                constexpr int K = 2, Z = 8;
-                const int zs = (x1 - x0 + step - 1) / step, quads = a.D / 4;
-                const int Rt = min(R - rt * C::kRows, C::kRows), all = min(a.H - hg * HG, HG) * Rt * quads;
-                for (int e0 = 0; e0 < all; e0 += K * kStreamThreads) {
-                    int from[K], at_row[K];
-                    f32x4_t acc[K];
-                    float mx[K], sum[K];
-#pragma unroll
-                    for (int k = 0; k < K; ++k) {
-                        const int e = min(e0 + k * kStreamThreads + tid, all - 1), y = e / quads;
-                        at_row[k] = y / Rt * C::kRows + y % Rt;
-                        from[k] = at_row[k] * DP + (e - y * quads) * 4;
-                        acc[k] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-                        mx[k] = kLowest;
-                        sum[k] = 0.0f;
-                    }
-                    for (int z0 = 0; z0 < zs; z0 += Z) {
-                        f32x4_t v[Z][K];
-                        uint64_t ml[Z][K];
-#pragma unroll
-                        for (int u = 0; u < Z; ++u)
-#pragma unroll
-                            for (int k = 0; k < K; ++k) {
-                                const int x = x0 + min(z0 + u, zs - 1) * step;
-                                ml[u][k] = __hip_atomic_load(ml_of(x, round) + at_row[k], __ATOMIC_RELAXED,
-                                                             __HIP_MEMORY_SCOPE_AGENT);
-                                v[u][k] = load_agent(part_of(x) + from[k]);
-                            }
-#pragma unroll
-                        for (int k = 0; k < K; ++k) {
-                            float top = mx[k];
-#pragma unroll
-                            for (int u = 0; u < Z; ++u) top = fmaxf(top, __uint_as_float((uint32_t)ml[u][k]));
-                            const float down = exp2_hw(mx[k] - top);
-                            mx[k] = top;
-                            sum[k] *= down;
-                            acc[k] *= down;
-#pragma unroll
-                            for (int u = 0; u < Z; ++u)
-                                if (z0 + u < zs) {
-                                    const float f = exp2_hw(__uint_as_float((uint32_t)ml[u][k]) - top);
-                                    sum[k] += __uint_as_float((uint32_t)(ml[u][k] >> 32)) * f;
-                                    acc[k] += v[u][k] * f;
-                                }
-                        }
-                    }
-#pragma unroll
-                    for (int k = 0; k < K; ++k) {
-                        if (e0 + k * kStreamThreads + tid >= all) break;
-                        const int d = from[k] - at_row[k] * DP;
-                        if (output) {
-                            const int h = at_row[k] / C::kRows, row = rt * C::kRows + at_row[k] % C::kRows;
-                            const int i = row / G, g = row - i * G;
-                            const float f = sum[k] == 0.0f ? 0.0f : 1.0f / sum[k];
-                            uint2 y;
-                            y.x = f32_to_bf16x2(acc[k][0] * f, acc[k][1] * f);
-                            y.y = f32_to_bf16x2(acc[k][2] * f, acc[k][3] * f);
-                            *reinterpret_cast<uint2*>(a.out + (int64_t)(first + i) * a.ld_out +
-                                                      (int64_t)((hg * HG + h) * G + g) * a.D + d) = y;
-                        } else {
-                            store_agent(part_of(x0) + from[k], acc[k]);
-                            if (d == 0)
-                                __hip_atomic_store(ml_of(x0, 1) + at_row[k], two_floats(mx[k], sum[k]), __ATOMIC_RELAXED,
-                                                   __HIP_MEMORY_SCOPE_AGENT);
-                        }
-                    }
-                }
-            };
-            if (last_of(tickets + slot_of(r0), min(run, parts - r0))) {
-                join(r0, min(r0 + run, parts), 1, 0, runs == 1);
-                if (runs > 1 && last_of(tickets + 2 * groups + w0, runs)) join(0, parts, run, 1, true);
-            }
-            __syncthreads();
+            parts.finish(a, line, sh);
         }
     }
 }
