@@ -528,7 +528,8 @@ spec_status spec_fp8_kv_cache_read(const uint8_t* k_cache, const uint8_t* v_cach
  *          overlap.
  * Requirements: T, B >= 0 (0: no-op), Hq, H, D, block_size > 0, max_blocks, num_blocks >= 0,
  * Hq % H == 0, ld_q and ld_out >= Hq*D, ld_tables >= max_blocks (SPEC_ERR_SHAPE); D % 8 == 0,
- * D <= 256, Hq <= 65535, T*Hq, B and num_blocks < 2^31, max_blocks*block_size < 2^31 - 65535 (SPEC_ERR_UNSUPPORTED); q, out,
+ * D <= 256, Hq <= 65535, T*Hq, B and num_blocks < 2^31, max_blocks*block_size < 2^31 - 65535,
+ * block_size*H*D < 2^32 (SPEC_ERR_UNSUPPORTED); q, out,
  * k_cache and v_cache 16-byte aligned, ld_q and ld_out multiples of 8, tree_mask 8-byte, the
  * tables, lengths and scales 4-byte aligned (SPEC_ERR_ALIGN); scale finite and > 0
  * (SPEC_ERR_VALUE); mode PER_ROW or PER_TENSOR (SPEC_ERR_ENUM).

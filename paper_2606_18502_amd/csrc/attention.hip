@@ -183,8 +183,27 @@ hipError_t launch_stream(const PagedArgs& a, void* workspace, hipStream_t stream
     return hipGetLastError();
 }
 
+template <int DP, int W>
+hipError_t launch_tiles(const PagedArgs& a, void* workspace, hipStream_t stream) {
+    constexpr int kRows = 32 * W, kKeys = TileShape_<DP>::kKeys;
+    constexpr int kLds = std::max(PagedTileShape<DP>::kLds, kRows * DP * 4);
+    const int64_t units = ((int64_t)a.T * (a.Hq / a.H) / kRows + a.B) * a.H;
+    const int64_t steps = units * std::max<int64_t>((a.max_len + kKeys - 1) / kKeys, 1);
+    const int grid = (int)std::max<int64_t>(std::min<int64_t>(steps / 2, tile_groups(DP, W)), 1);
+    float* const part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace) + kAttnTicketBytes);
+    unsigned int* const tickets = reinterpret_cast<unsigned int*>(workspace);
+    if (a.per_tensor)
+        hipLaunchKernelGGL((paged_tile_kernel<DP, true, W>), dim3(grid), dim3(64 * W), kLds, stream, a, part, tickets, grid, 2, 3);
+    else
+        hipLaunchKernelGGL((paged_tile_kernel<DP, false, W>), dim3(grid), dim3(64 * W), kLds, stream, a, part, tickets, grid, 2, 3);
+    return hipGetLastError();
+}
+
 template <int DP>
 hipError_t launch_stream_rows(const PagedPlan& p, const PagedArgs& a, void* workspace, hipStream_t stream) {
+    if constexpr (DP == 128)
+        if (p.tile_waves == 8) return launch_tiles<DP, 8>(a, workspace, stream);
+    if (p.tile_waves == 4) return launch_tiles<DP, 4>(a, workspace, stream);
     if (p.hg == 1)
         return p.nq == 1 ? launch_stream<DP, 1, 1>(a, workspace, stream) : launch_stream<DP, 2, 1>(a, workspace, stream);
     if (p.hg == 2)
@@ -212,9 +231,11 @@ hipError_t launch_paged_attention(const PagedArgs& given, void* workspace, hipSt
 
 hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t stream) {
     const int64_t G = a.Hq / a.H, slots = (int64_t)a.T * G / 128 + a.B;
-    if (a.D <= 128 && slots * a.H * 256 <= 0xffffffffll) {
+    if (slots * a.H * 256 <= 0xffffffffll) {
         const dim3 grid((unsigned)(slots * a.H)), block(256);
-        if (a.D <= 64)
+        if (a.D > 128)
+            hipLaunchKernelGGL(prompt_tile_kernel<256>, grid, block, TileShape_<256>::kLds, stream, a, (int)slots);
+        else if (a.D <= 64)
             hipLaunchKernelGGL(prompt_tile_kernel<64>, grid, block, TileShape_<64>::kLds, stream, a, (int)slots);
         else
             hipLaunchKernelGGL(prompt_tile_kernel<128>, grid, block, TileShape_<128>::kLds, stream, a, (int)slots);

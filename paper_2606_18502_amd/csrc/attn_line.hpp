@@ -3,7 +3,7 @@
 // A unit is (sequence, ROWS rows of a KV head's group, HG KV heads); its cost is
 // its number of key steps, and `extra` for its beginning (queries, first loads,
 // what is stored at its end).  The units lie on one line in the order
-// sequence, row tile, heads, and the workgroups cut it into equal ranges, whatever
+// sequence, heads, row tile (a head's tiles read the same keys), and the workgroups cut it into equal ranges, whatever
 // the sequences' lengths, which only the device knows.  A range covers whole units and parts of
 // at most two.  The parts of a unit are joined by the workgroup that stores the
 // last of them, found by a ticket per unit at the workgroup where the unit
@@ -123,8 +123,9 @@ struct Line {
                 continue;
             }
             const int unit = uniform((int)((pos - base) / (steps + extra)));
-            rt = unit / nhg;
-            hg = unit - rt * nhg;
+            const int tiles = (int)(((int64_t)n * (a.Hq / a.H) + ROWS - 1) / ROWS);
+            hg = unit / tiles;
+            rt = unit - hg * tiles;
             u0 = base + (int64_t)unit * (steps + extra) + extra;
             s_in = (int)max(pos - u0, (int64_t)0);
             const int s_out = (int)min(hi - u0, (int64_t)steps);

@@ -76,7 +76,7 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     __shared__ LineShared<64 * W> sh;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int G = a.Hq / a.H, NHG = (a.H + HG - 1) / HG;
+    const int G = a.Hq / a.H;
     const int q16 = lane & 15, qd = lane >> 4;
 
     Line<64 * W, C::kRows, C::kStep> line;
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
     const int bs = a.block_size, step_q = C::kStep / bs, step_r = C::kStep % bs;
     const int last_block = max(a.max_len / bs - 1, 0);
     const float* const scales = lane < 32 ? a.k_scale : a.v_scale;
-    const uint64_t page_rows = (uint64_t)bs * (uint32_t)a.H;
+    const uint32_t page_rows = bs * a.H, page_bytes = page_rows * a.D;          // (a page has less than 4 GiB of codes)
     const float c2 = a.scale * 1.4426950408889634f;
 
     while (line.next(a, sh)) {
@@ -159,9 +159,9 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
             const auto prepare = [&](int t) -> uint32_t {            // byte offsets and scales of tile t; which keys there are
                 const int page = (int)tab[(t % S) * 64 + lane];
                 const bool there = next_key + key < L && page >= 0 && page < a.num_blocks;
-                const uint32_t pg = there ? page : 0, of = there ? off_p : 0;
-                const uint64_t row = pg * page_rows + (of * (uint64_t)(uint32_t)a.H + (uint32_t)head);
-                if (lane < 32) offs[key] = (int64_t)(row * (uint32_t)a.D);
+                const uint32_t pg = there ? page : 0, in = (there ? off_p : 0) * a.H + head;
+                const uint64_t row = (uint64_t)pg * page_rows + in;
+                if (lane < 32) offs[key] = (int64_t)((uint64_t)pg * page_bytes + in * (uint32_t)a.D);
                 load_lds4(scales + (a.per_tensor ? 0 : row), ring_at + (t % S) * C::kStage + 2 * C::kTile);
                 off_p += step_r;
                 if (off_p >= bs) off_p -= bs;

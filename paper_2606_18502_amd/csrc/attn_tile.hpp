@@ -21,7 +21,7 @@
 
 #include <type_traits>
 
-#include "attn_common.hpp"
+#include "attn_line.hpp"
 
 namespace specfp8 {
 
@@ -53,18 +53,16 @@ template <int DP>
 struct RowState {
     f32x16_t o[DP / 32];
     float m, l;
-    uint64_t plus, minus;         // channels (16 * block + i) that +inf or NaN, and -inf or NaN, values reached
-    static_assert(DP <= 128, "64 marks");
+    uint64_t plus[(DP + 127) / 128], minus[(DP + 127) / 128];     // channels (16 * block + i) that +inf or NaN, and
+                                                                  // -inf or NaN, values reached
 };
 
 // Two bf16 halves that are infinite or NaN: 0x8000 in each.
 __device__ __forceinline__ uint32_t not_finite(uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 
-// The keys of a tile that a row sees when these are its first `visible` ones, as a lane holds them: bit
-// 32 kb + 8 (i/4) + i % 4 is key 32 kb + 8 (i/4) + 4 (lane/32) + i % 4.
-__device__ __forceinline__ uint64_t seen_keys(int visible) {
-    const int d = visible - 4 * (int)((threadIdx.x >> 5) & 1);
-    return d <= 0 ? 0 : (d >= 64 ? ~0ull : (1ull << d) - 1);
+// The first `visible` keys of a tile, as bits.
+__device__ __forceinline__ uint64_t first_keys(int visible) {
+    return visible <= 0 ? 0 : (visible >= 64 ? ~0ull : (1ull << visible) - 1);
 }
 
 // The second product's operand: 8 keys (k-slots) of one channel per lane; a lane of 16 addresses 4 channels
@@ -87,10 +85,11 @@ struct ValueReads {
 };
 
 // One tile of 64 keys at LDS `kt`, `vt` for a wave's 32 rows.  full: every row sees all of it; otherwise a row
-// sees its first `visible` keys.
-template <int DP>
+// sees the keys of `row_sees`.  SCALED: keys and values have scales of their own in LDS, the keys' with c2 in them.
+template <int DP, bool SCALED>
 __device__ __forceinline__ void attend_tile(RowState<DP>& st, const bf16x8_t (&q)[DP / 16], uint32_t kt, uint32_t vt,
-                                            int visible, bool full, float c2) {
+                                            uint64_t row_sees, bool full, float c2, const float* k_scales,
+                                            const float* v_scales) {
     using C = TileShape_<DP>;
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
     // ---- scores
@@ -109,8 +108,16 @@ __device__ __forceinline__ void attend_tile(RowState<DP>& st, const bf16x8_t (&q
             s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[ks], s[kb], 0, 0, 0);
         }
     }
+    if constexpr (SCALED) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const f32x4_t f = *reinterpret_cast<const f32x4_t*>(k_scales + 8 * x + 4 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[x >> 2][4 * (x & 3) + e] *= f[e];
+        }
+    }
     if (!full) {
-        const uint64_t seen = seen_keys(visible);
+        const uint64_t seen = row_sees >> (4 * h);           // bit 32 kb + 8 (i/4) + i % 4: key 4 h further
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -122,7 +129,7 @@ __device__ __forceinline__ void attend_tile(RowState<DP>& st, const bf16x8_t (&q
     for (int i = 1; i < 16; ++i) top = fmaxf(top, s[0][i]);
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, s[1][i]);
-    top *= c2;
+    if constexpr (!SCALED) top *= c2;
     if (__ballot(top > st.m + kLazy)) {
         const float mx = fmaxf(st.m, max_halves(top));
         const float down = exp2_hw(st.m - mx);
@@ -140,8 +147,20 @@ __device__ __forceinline__ void attend_tile(RowState<DP>& st, const bf16x8_t (&q
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int i = 8 * (u & 1) + 2 * e;
-            const float a = exp2_hw(fmaf(s[u >> 1][i], c2, -st.m)), b = exp2_hw(fmaf(s[u >> 1][i + 1], c2, -st.m));
+            float a, b;
+            if constexpr (SCALED) {
+                a = exp2_hw(s[u >> 1][i] - st.m);
+                b = exp2_hw(s[u >> 1][i + 1] - st.m);
+            } else {
+                a = exp2_hw(fmaf(s[u >> 1][i], c2, -st.m));
+                b = exp2_hw(fmaf(s[u >> 1][i + 1], c2, -st.m));
+            }
             sum += a + b;
+            if constexpr (SCALED) {
+                const float2 f = *reinterpret_cast<const float2*>(v_scales + 16 * u + 8 * (e >> 1) + 4 * h + 2 * (e & 1));
+                a *= f.x;
+                b *= f.y;
+            }
             w[e] = f32_to_bf16x2(a, b);
         }
         p[u] = __builtin_bit_cast(bf16x8_t, w);
@@ -161,9 +180,9 @@ __device__ __forceinline__ void attend_tile(RowState<DP>& st, const bf16x8_t (&q
 // some row sees in part such values count 0 in the sums (clean_tile), and (keys that hold one) x (keys
 // that a row sees), as products of ones, mark the channels that they reach (mark_tile).
 template <int DP>
-__device__ __forceinline__ void mark_tile(uint32_t vt, int visible, uint64_t& plus, uint64_t& minus) {
+__device__ __forceinline__ void mark_tile(RowState<DP>& st, uint32_t vt, uint64_t row_sees) {
     using C = TileShape_<DP>;
-    const uint64_t seen = seen_keys(visible);
+    const uint64_t seen = row_sees >> (4 * ((threadIdx.x >> 5) & 1));
     const ValueReads<DP> values(vt);
 #pragma unroll 1
     for (int u = 0; u < 4; ++u) {
@@ -197,19 +216,22 @@ __device__ __forceinline__ void mark_tile(uint32_t vt, int visible, uint64_t& pl
                 x |= (uint32_t)(hp[i] > 0.0f) << i;
                 y |= (uint32_t)(hm[i] > 0.0f) << i;
             }
-            plus |= (uint64_t)x << (16 * d);
-            minus |= (uint64_t)y << (16 * d);
+#pragma unroll
+            for (int z = 0; z < (DP + 127) / 128; ++z) {
+                st.plus[z] |= d >> 2 == z ? (uint64_t)x << (16 * (d & 3)) : 0;
+                st.minus[z] |= d >> 2 == z ? (uint64_t)y << (16 * (d & 3)) : 0;
+            }
         }
     }
 }
 
-// This thread's part of the tile: whether it holds such values / without them.
+// This thread's part of the tile: whether it holds such values / without them.  16 bytes of key
+// (threadIdx.x + 256 x) / (DP / 8) at a time.
 template <int DP>
 __device__ __forceinline__ bool wild_part(const uint8_t* tile) {
     uint32_t any = 0;
-#pragma unroll
-    for (int x = 0; x < TileShape_<DP>::kTile / 4096; ++x) {
-        const u32x4_t v = *reinterpret_cast<const u32x4_t*>(tile + x * 4096 + threadIdx.x * 16);
+    for (int x = threadIdx.x * 16; x < TileShape_<DP>::kTile; x += blockDim.x * 16) {
+        const u32x4_t v = *reinterpret_cast<const u32x4_t*>(tile + x);
         any |= not_finite(v[0]) | not_finite(v[1]) | not_finite(v[2]) | not_finite(v[3]);
     }
     return any != 0;
@@ -217,8 +239,8 @@ __device__ __forceinline__ bool wild_part(const uint8_t* tile) {
 template <int DP>
 __device__ __forceinline__ void clean_part(uint8_t* tile) {
 #pragma unroll 1
-    for (int x = 0; x < TileShape_<DP>::kTile / 4096; ++x) {
-        u32x4_t* const at = reinterpret_cast<u32x4_t*>(tile + x * 4096 + threadIdx.x * 16);
+    for (int x = threadIdx.x * 16; x < TileShape_<DP>::kTile; x += blockDim.x * 16) {
+        u32x4_t* const at = reinterpret_cast<u32x4_t*>(tile + x);
         u32x4_t v = *at;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] &= ~((not_finite(v[e]) >> 15) * 0xffffu);
@@ -226,11 +248,24 @@ __device__ __forceinline__ void clean_part(uint8_t* tile) {
     }
 }
 
+// Keys that are not there have values 0; keys whose value scale is infinite or NaN have NaN values and no weight.
+template <int DP>
+__device__ __forceinline__ void settle_part(uint8_t* tile, uint64_t there, const float* v_scales) {
+#pragma unroll 1
+    for (int x = threadIdx.x * 16; x < TileShape_<DP>::kTile; x += blockDim.x * 16) {
+        const int key = x / (2 * DP);
+        u32x4_t* const at = reinterpret_cast<u32x4_t*>(tile + x);
+        if (!((there >> key) & 1)) *at = u32x4_t{0, 0, 0, 0};
+        else if (v_scales && !(fabsf(v_scales[key]) < INFINITY)) *at = u32x4_t{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+    }
+}
+
 template <int DP>
 __device__ __forceinline__ void begin_rows(RowState<DP>& st) {
     st.m = kLowest;
     st.l = 0.0f;
-    st.plus = st.minus = 0;
+#pragma unroll
+    for (int z = 0; z < (DP + 127) / 128; ++z) st.plus[z] = st.minus[z] = 0;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
@@ -241,21 +276,41 @@ __device__ __forceinline__ void begin_rows(RowState<DP>& st) {
 template <int DP>
 __device__ __forceinline__ void end_rows(RowState<DP>& st) {
     st.l = sum_halves(st.l);
-    if (__ballot((st.plus | st.minus) != 0)) {
+    uint64_t any = 0;
+#pragma unroll
+    for (int z = 0; z < (DP + 127) / 128; ++z) any |= st.plus[z] | st.minus[z];
+    if (__ballot(any != 0)) {
 #pragma unroll
         for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const bool a = (st.plus >> (16 * d + i)) & 1, b = (st.minus >> (16 * d + i)) & 1;
-                if (a) st.o[d][i] += INFINITY;
-                if (b) st.o[d][i] -= INFINITY;
+                const int at = 16 * (d & 3) + i;
+                if ((st.plus[d >> 2] >> at) & 1) st.o[d][i] += INFINITY;
+                if ((st.minus[d >> 2] >> at) & 1) st.o[d][i] -= INFINITY;
             }
     }
 }
 
+// The rows' results as bf16: channels 32 d + 8 x + 4 (lane/32) .. of this lane's row, `dst` its first channel.
+template <int DP>
+__device__ __forceinline__ void store_rows(const RowState<DP>& st, uint16_t* dst, int D, float scale) {
+    const float inv = st.l == 0.0f ? 0.0f : scale / st.l;
+    dst += 4 * ((threadIdx.x >> 5) & 1);
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+            if (32 * d + 8 * x < D) {
+                uint2 y;
+                y.x = f32_to_bf16x2(st.o[d][4 * x] * inv, st.o[d][4 * x + 1] * inv);
+                y.y = f32_to_bf16x2(st.o[d][4 * x + 2] * inv, st.o[d][4 * x + 3] * inv);
+                *reinterpret_cast<uint2*>(dst + 32 * d + 8 * x) = y;
+            }
+}
+
 // ---- prompts: K and V straight from bf16 rows ------------------------------------
 template <int DP>
-__global__ __launch_bounds__(256, 2) void prompt_tile_kernel(PromptArgs a, int slots) {
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void prompt_tile_kernel(PromptArgs a, int slots) {
     using C = TileShape_<DP>;
     extern __shared__ __attribute__((aligned(1024))) uint8_t tile_smem[];
     const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), h = lane >> 5, l32 = lane & 31;
@@ -306,15 +361,34 @@ __global__ __launch_bounds__(256, 2) void prompt_tile_kernel(PromptArgs a, int s
     const int chunks = a.D / 8, ld_key = lane / kChunks, ld_slot = lane % kChunks;
     const uint16_t* const k_rows = a.k + (int64_t)first * a.ld_k + (int64_t)head * a.D;
     const uint16_t* const v_rows = a.v + (int64_t)first * a.ld_v + (int64_t)head * a.D;
+    const uint16_t *k_at[C::kLoads], *v_at[C::kLoads];                          // of the next tile to load
+    int k_part[C::kLoads], v_part[C::kLoads];
+#pragma unroll
+    for (int x = 0; x < C::kLoads; ++x) {
+        const int r = (4 * x + w) * kPer + ld_key;
+        const int ck = ld_slot ^ tile_k_swizzle<DP>(r), cv = ld_slot ^ tile_v_swizzle<DP>(r);
+        k_part[x] = ck < chunks ? ck * 8 : 0;                                  // (past the head's end: any; queries are 0)
+        v_part[x] = cv < chunks ? cv * 8 : 0;
+        k_at[x] = k_rows + r * a.ld_k + k_part[x];
+        v_at[x] = v_rows + r * a.ld_v + v_part[x];
+    }
+    const int64_t k_step = C::kKeys * a.ld_k, v_step = C::kKeys * a.ld_v;
     const auto stage = [&](int t) {
         const uint32_t to = smem + (t & 1) * 2 * C::kTile;
+        if ((t + 1) * C::kKeys > n) {                                          // past the end: the last key again
+#pragma unroll
+            for (int x = 0; x < C::kLoads; ++x) {
+                const int64_t key = min(t * C::kKeys + (4 * x + w) * kPer + ld_key, n - 1);
+                k_at[x] = k_rows + key * a.ld_k + k_part[x];
+                v_at[x] = v_rows + key * a.ld_v + v_part[x];
+            }
+        }
 #pragma unroll
         for (int x = 0; x < C::kLoads; ++x) {
-            const int part = 4 * x + w, r = part * kPer + ld_key;
-            const int64_t key = min(t * C::kKeys + r, n - 1);                   // (past the end: the last key again)
-            const int ck = ld_slot ^ tile_k_swizzle<DP>(r), cv = ld_slot ^ tile_v_swizzle<DP>(r);
-            load_lds16(k_rows + key * a.ld_k + (ck < chunks ? ck * 8 : 0), to + part * 1024);
-            load_lds16(v_rows + key * a.ld_v + (cv < chunks ? cv * 8 : 0), to + C::kTile + part * 1024);
+            load_lds16(k_at[x], to + (4 * x + w) * 1024);
+            load_lds16(v_at[x], to + C::kTile + (4 * x + w) * 1024);
+            k_at[x] += k_step;
+            v_at[x] += v_step;
         }
     };
     RowState<DP> st;
@@ -331,29 +405,238 @@ __global__ __launch_bounds__(256, 2) void prompt_tile_kernel(PromptArgs a, int s
         const int k0 = t * C::kKeys;
         uint8_t* const values = tile_smem + (t & 1) * 2 * C::kTile + C::kTile;
         if (k0 + C::kKeys - 1 > first_token && __syncthreads_or(wild_part<DP>(values))) {
-            mark_tile<DP>(kt + C::kTile, i + 1 - k0, st.plus, st.minus);
+            mark_tile(st, kt + C::kTile, first_keys(i + 1 - k0));
             __syncthreads();
             clean_part<DP>(values);
             __syncthreads();
         }
-        if (k0 <= wave_last) attend_tile(st, q, kt, kt + C::kTile, i + 1 - k0, k0 + C::kKeys - 1 <= wave_first, c2);
+        if (k0 <= wave_last) 
+            attend_tile<DP, false>(st, q, kt, kt + C::kTile, first_keys(i + 1 - k0), k0 + C::kKeys - 1 <= wave_first, c2,
+                                   nullptr, nullptr);
         wait_loads<0>();
         __syncthreads();
     }
     end_rows(st);
-    if (!there) return;
-    const float inv = st.l == 0.0f ? 0.0f : 1.0f / st.l;
-    uint16_t* const dst = a.out + (int64_t)(first + i) * a.ld_out + (int64_t)(head * G + g) * a.D + 4 * h;
+    if (there) store_rows(st, a.out + (int64_t)(first + i) * a.ld_out + (int64_t)(head * G + g) * a.D, a.D, 1.0f);
+}
+
+// ---- new rows over the paged FP8 cache --------------------------------------------
+// Work: attn_line.hpp; a unit is (sequence, 32 W rows, one KV head), a step 64 keys.  The codes of the next tile
+// are loaded to registers while a tile is attended to, and written to LDS as bf16 (exact) after it; the table entries of
+// the tile after that travel meanwhile.  PT: one scale for the keys and one for the values.
+// A wave's rows of a part leave through its corner of LDS, so that a store instruction writes whole rows (stored by
+// 16 bytes of 32 rows each, a part took 22 us in place of 10): quads (four channels) of row r lie at slot
+// quad ^ r, which spreads a column of them over the banks.
+template <int DP>
+struct RowBox {
+    static constexpr int kQuads = DP / 4;
+    static __device__ __forceinline__ int at(int row, int quad) { return row * kQuads + (quad ^ (row & (kQuads - 1))); }
+    // the sums of `rows` rows to a part (through to memory)
+    static __device__ __forceinline__ void store_part(const f32x4_t* box, float* to, int rows) {
+        const int lane = threadIdx.x & 63;
+        const float2* const pairs = reinterpret_cast<const float2*>(box);
+        uint64_t* const dst = reinterpret_cast<uint64_t*>(to);
+#pragma unroll 4
+        for (int x = lane; x < rows * (DP / 2); x += 64) {
+            const int r = x / (DP / 2), c = x % (DP / 2);
+            const float2 v = pairs[2 * at(r, c >> 1) + (c & 1)];
+            __hip_atomic_store(dst + x, two_floats(v.x, v.y), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    }
+};
+
+template <int DP>
+struct PagedTileShape {
+    static constexpr int kScales = 4 * TileShape_<DP>::kTile;                  // two tiles' 64 + 64 scales and masks
+    static constexpr int kLds = kScales + 2 * (512 + 16);
+};
+
+template <int DP, bool PT, int W>
+__global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_tile_kernel(PagedArgs a, float* part, unsigned int* tickets,
+                                                                            int groups, int min_steps, int extra) {
+    using C = TileShape_<DP>;
+    constexpr int kThreads = 64 * W, kRows = 32 * W;
+    using PartsT = Parts<kThreads, kRows, C::kKeys, 1, DP>;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t tile_smem[];
+    __shared__ LineShared<kThreads> sh;
+    const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), h = lane >> 5, l32 = lane & 31;
+    const int G = a.Hq / a.H;
+    Line<kThreads, kRows, C::kKeys> line;
+    if (!line.begin(a, sh, 1, groups, min_steps, extra)) return;
+
+    const uint32_t smem = uniform((int)lds_at(tile_smem));
+    float* const scales = reinterpret_cast<float*>(tile_smem + PagedTileShape<DP>::kScales);      // [2][128]
+    uint64_t* const masks = reinterpret_cast<uint64_t*>(scales + 256);                            // [2]
+    // loads: 16 codes of key tid/kChunks + x kKeys16; table entries of those keys, and of the key whose scale this is
+    constexpr int kChunks = DP / 16, kPer = kThreads / kChunks, NL = 64 / kPer;
+    const int ld_key = tid / kChunks, ld_chunk = tid % kChunks, sc_key = tid & 63;
+    const int src_chunk = ld_chunk * 16 < a.D ? ld_chunk * 16 : 0;             // (past the head's end: any; queries are 0)
+    // (a page has less than 4 GiB of codes)
+    const int bs = a.block_size, step_q = C::kKeys / bs, step_r = C::kKeys % bs;
+    const uint32_t row_bytes = a.H * a.D, page_bytes = bs * row_bytes, page_rows = bs * a.H;
+    const int last_block = max(a.max_len / bs - 1, 0);
+    const float c2 = a.scale * 1.4426950408889634f * (PT ? a.k_scale[0] : 1.0f);
+
+    while (line.next(a, sh)) {
+        const int n = line.n, L = line.L, first = line.first, head = line.hg;
+        const int64_t R = (int64_t)n * G, row0 = (int64_t)line.rt * kRows;
+        // the rows
+        const int64_t row = row0 + 32 * w + l32;
+        const bool there = row < R;
+        const int i = there ? (int)(row / G) : 0, g = there ? (int)(row - (int64_t)i * G) : 0;
+        const uint16_t* const src = a.q + (int64_t)(first + i) * a.ld_q + (int64_t)(head * G + g) * a.D;
+        bf16x8_t q[C::KS];
 #pragma unroll
-    for (int d = 0; d < C::DB; ++d)
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-            if (32 * d + 8 * x < a.D) {
-                uint2 y;
-                y.x = f32_to_bf16x2(st.o[d][4 * x] * inv, st.o[d][4 * x + 1] * inv);
-                y.y = f32_to_bf16x2(st.o[d][4 * x + 2] * inv, st.o[d][4 * x + 3] * inv);
-                *reinterpret_cast<uint2*>(dst + 32 * d + 8 * x) = y;
+        for (int ks = 0; ks < C::KS; ++ks) {
+            const int d = 16 * ks + 8 * h;
+            u32x4_t v = *reinterpret_cast<const u32x4_t*>(src + min(d, a.D - 8));
+            if (d >= a.D) v = u32x4_t{0, 0, 0, 0};
+            q[ks] = __builtin_bit_cast(bf16x8_t, v);
+        }
+        // what they see: tokens up to lim, or a tree's; all of a tile up to some token; none past another
+        const int lim = a.tree ? L - 1 : L - n + i;
+        const uint64_t nodes = a.tree && there && i > 0 ? a.tree[(int64_t)line.b * a.N + i - 1] : 0;
+        const auto first_of = [&](int64_t r) { return (int)min(r / G, (int64_t)n - 1); };
+        const int all_see = a.tree ? L - a.N - 1 : L - n + uniform(first_of(row0));
+        const int wave_all = a.tree ? all_see : L - n + uniform(first_of(row0 + 32 * w));
+        const int wave_last = row0 + 32 * w >= R ? -1 : a.tree ? L - 1 : L - n + uniform(first_of(min(row0 + 32 * w + 31, R - 1)));
+        const int last = a.tree ? L - 1 : L - n + uniform(first_of(min(row0 + kRows, R) - 1));
+        const int count = min(line.count, (last >> 6) + 1 - line.s_in);        // (tiles that some row sees)
+        const auto sees = [&](int k0) -> uint64_t {
+            uint64_t m = first_keys(lim + 1 - k0);
+            if (a.tree) {
+                const int f = k0 - (L - a.N);                                  // node number of the tile's first key
+                if (f >= 0) m &= f < 64 ? nodes >> f : 0;
+                else if (f > -64) m &= nodes << -f | ((1ull << -f) - 1);
             }
+            return m;
+        };
+
+        // ---- loads
+        const int32_t* const table = a.max_len > 0 ? a.tables + (int64_t)line.b * a.ld_tables : a.kv_lens;
+        int blk[NL + 1], off[NL + 1], page[NL + 1], in_page[NL + 1];
+        int key0 = line.s_in * C::kKeys, code_key0 = key0;                     // first key of the tile to look up, to load
+#pragma unroll
+        for (int x = 0; x <= NL; ++x) {
+            const int k = key0 + (x < NL ? ld_key + x * kPer : sc_key);
+            blk[x] = k / bs;
+            off[x] = k - blk[x] * bs;
+        }
+        const auto look_up = [&]() {
+#pragma unroll
+            for (int x = 0; x <= NL; ++x) {
+                page[x] = table[min(blk[x], last_block)];
+                in_page[x] = off[x];
+                off[x] += step_r;
+                blk[x] += step_q;
+                if (off[x] >= bs) {
+                    off[x] -= bs;
+                    ++blk[x];
+                }
+            }
+        };
+        const uint8_t *const k_from = a.k_cache + src_chunk, *const v_from = a.v_cache + src_chunk;
+        u32x4_t kc[NL], vc[NL];
+        float scale = 0.0f;
+        bool scale_there = false;
+        uint64_t present = 0;                                                  // (wave 0) the keys that there are
+        const auto load = [&]() {
+#pragma unroll
+            for (int x = 0; x <= NL; ++x) {
+                const int k = code_key0 + (x < NL ? ld_key + x * kPer : sc_key);
+                const bool ok = k < L && page[x] >= 0 && page[x] < a.num_blocks;
+                const uint32_t pg = ok ? page[x] : 0, in = ok ? in_page[x] : 0;           // (not there: some row)
+                if (x < NL) {
+                    const uint64_t r = (uint64_t)pg * page_bytes + (in * row_bytes + head * a.D);
+                    kc[x] = *reinterpret_cast<const u32x4_t*>(k_from + r);
+                    vc[x] = *reinterpret_cast<const u32x4_t*>(v_from + r);
+                } else {
+                    const uint64_t r = (uint64_t)pg * page_rows + (in * a.H + head);
+                    present = __ballot(ok);
+                    if constexpr (!PT) {
+                        scale_there = ok;
+                        scale = (tid & 64 ? a.v_scale : a.k_scale)[r];
+                    }
+                }
+            }
+            code_key0 += C::kKeys;
+        };
+        const auto write = [&](int t) {
+            uint8_t* const to = tile_smem + (t & 1) * 2 * C::kTile;
+#pragma unroll
+            for (int x = 0; x < NL; ++x) {
+                const int r = ld_key + x * kPer;
+                bf16x8_t* const krow = reinterpret_cast<bf16x8_t*>(to + r * C::kRowBytes);
+                bf16x8_t* const vrow = reinterpret_cast<bf16x8_t*>(to + C::kTile + r * C::kRowBytes);
+                const int fk = tile_k_swizzle<DP>(r), fv = tile_v_swizzle<DP>(r);
+                krow[(2 * ld_chunk) ^ fk] = codes_to_bf16(kc[x][0], kc[x][1]);
+                krow[(2 * ld_chunk + 1) ^ fk] = codes_to_bf16(kc[x][2], kc[x][3]);
+                vrow[(2 * ld_chunk) ^ fv] = codes_to_bf16(vc[x][0], vc[x][1]);
+                vrow[(2 * ld_chunk + 1) ^ fv] = codes_to_bf16(vc[x][2], vc[x][3]);
+            }
+            if (tid == 0) masks[t & 1] = present;
+            if constexpr (!PT)
+                if (tid < 128) scales[(t & 1) * 128 + tid] = scale_there ? (tid < 64 ? scale * c2 : scale) : 0.0f;
+        };
+
+        RowState<DP> st;
+        begin_rows(st);
+        if (count > 0) {
+            look_up();
+            load();
+            if (count > 1) look_up();
+            write(0);
+            __syncthreads();
+        }
+        for (int t = 0; t < count; ++t) {
+            if (t + 1 < count) load();
+            if (t + 2 < count) look_up();
+            const uint32_t kt = smem + (t & 1) * 2 * C::kTile;
+            const int k0 = (line.s_in + t) * C::kKeys;
+            const uint64_t mask = uniform((int64_t)masks[t & 1]);
+            uint8_t* const values = tile_smem + (t & 1) * 2 * C::kTile + C::kTile;
+            float* const sc = scales + (t & 1) * 128;
+            if (mask != ~0ull || k0 + C::kKeys - 1 > all_see) {
+                // (not there, or seen in part)
+                const bool odd = !PT && tid < 64 && !(fabsf(sc[64 + tid]) < INFINITY);
+                if (__syncthreads_or(mask != ~0ull || odd || wild_part<DP>(values))) {
+                    settle_part<DP>(values, mask, PT ? nullptr : sc + 64);
+                    __syncthreads();
+                    if (odd) sc[64 + tid] = 0.0f;
+                    const bool wild = __syncthreads_or(wild_part<DP>(values));
+                    if (wild) {
+                        mark_tile(st, kt + C::kTile, sees(k0) & mask);
+                        __syncthreads();
+                        clean_part<DP>(values);
+                    }
+                    __syncthreads();
+                }
+            }
+            if (k0 <= wave_last)
+                attend_tile<DP, !PT>(st, q, kt, kt + C::kTile, sees(k0) & mask,
+                                     mask == ~0ull && k0 + C::kKeys - 1 <= wave_all, c2, sc, sc + 64);
+            if (t + 1 < count) write(t + 1);
+            __syncthreads();
+        }
+        end_rows(st);
+        const float v_scale = PT ? a.v_scale[0] : 1.0f;
+        if (line.whole()) {
+            if (there) store_rows(st, a.out + (int64_t)(first + i) * a.ld_out + (int64_t)(head * G + g) * a.D, a.D, v_scale);
+        } else {
+            const PartsT parts(line, part, tickets, groups);
+            f32x4_t* const box = reinterpret_cast<f32x4_t*>(tile_smem + w * 32 * DP * 4);
+#pragma unroll
+            for (int d = 0; d < C::DB; ++d)
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    box[RowBox<DP>::at(l32, 8 * d + 2 * x + h)] =
+                        f32x4_t{st.o[d][4 * x], st.o[d][4 * x + 1], st.o[d][4 * x + 2], st.o[d][4 * x + 3]} * v_scale;
+            RowBox<DP>::store_part(box, parts.sums(parts.me) + 32 * w * DP,
+                                      (int)max(min(R - row0 - 32 * w, (int64_t)32), (int64_t)0));
+            if (there && h == 0) parts.store_ml(32 * w + l32, st.m, st.l);
+            parts.finish(a, line, sh);
+        }
+    }
 }
 
 }  // namespace

@@ -6,6 +6,7 @@
 
 #include "kernels.hpp"
 #include "plan.hpp"
+#include <stdlib.h>
 
 namespace specfp8 {
 
@@ -187,10 +188,16 @@ AcceptPlan plan_accept(int64_t B, int64_t k, int64_t V) {
 }
 
 PagedPlan plan_paged(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D) {
-    PagedPlan p{0, 1, 1, kAttnTicketBytes};
+    PagedPlan p{0, 0, 1, 0, kAttnTicketBytes};
     if (D % 16 != 0) return p;
     p.dp = D <= 64 ? 64 : (D <= 128 ? 128 : 256);
     const int64_t rows = (T + B - 1) / B * (Hq / H);       // of an average sequence and one KV head
+    static const int64_t lim = getenv("AR") ? atoi(getenv("AR")) : 32, lim8 = getenv("A8") ? atoi(getenv("A8")) : 128;
+    if (rows > lim) {
+        p.tile_waves = p.dp == 128 && rows > lim8 ? 8 : 4;
+        p.bytes += (size_t)tile_groups(p.dp, p.tile_waves) * 2 * 32 * p.tile_waves * (p.dp + 4) * sizeof(float);
+        return p;
+    }
     p.nq = rows <= 16 ? 1 : 2;
     p.hg = H == 1 ? 1 : (H == 2 || p.nq == 2 ? 2 : 4);
     p.bytes += (size_t)kAttnGroups * 2 * p.hg * p.nq * 16 * (p.dp + 4) * sizeof(float);

@@ -106,7 +106,7 @@ spec_status check_paged_attention(const void* q, int64_t ld_q, const void* k_cac
     if (block_size <= 0 || num_blocks < 0 || max_blocks < 0 || ld_tables < max_blocks) return SPEC_ERR_SHAPE;
     if (num_blocks > kMaxGrid || block_size > kMaxTokens || max_blocks > kMaxTokens / block_size)
         return SPEC_ERR_UNSUPPORTED;
-    if (num_blocks > INT64_MAX / (block_size * H) / D || (B > 0 && ld_tables > INT64_MAX / 4 / B))
+    if (block_size > 0xffffffffLL / (H * D) || num_blocks > INT64_MAX / (block_size * H) / D || (B > 0 && ld_tables > INT64_MAX / 4 / B))
         return SPEC_ERR_UNSUPPORTED;
     if (ld_q < Hq * D || ld_out < Hq * D) return SPEC_ERR_SHAPE;
     if ((tree_mask == nullptr) != (N == 0)) return SPEC_ERR_SHAPE;
