@@ -170,45 +170,44 @@ __global__ __launch_bounds__(kRowThreads) void attention_row_kernel(PagedArgs a,
 namespace {
 
 template <int DP, int NQ, int HG>
-hipError_t launch_stream(const PagedArgs& a, void* workspace, hipStream_t stream) {
+hipError_t launch_stream(const PagedPlan& p, const PagedArgs& a, void* workspace, hipStream_t stream) {
     using C = StreamShape<DP, NQ, HG, 2, 4>;
-    // The lengths are the device's: never more workgroups than there are steps where every sequence fills its table,
-    // at two steps each (fewer are not worth a join).
+    // The lengths are the device's: never more workgroups than there are cells where every sequence fills its table.
     const int64_t units = ((int64_t)a.T * (a.Hq / a.H) / C::kRows + a.B) * ((a.H + HG - 1) / HG);
-    const int64_t steps = units * std::max<int64_t>((a.max_len + C::kStep - 1) / C::kStep, 1);
-    const int grid = (int)std::max<int64_t>(std::min<int64_t>(steps / 2, kAttnGroups), 1);
+    const int64_t cells = units * std::max<int64_t>(((a.max_len + C::kStep - 1) / C::kStep + 1) / kCell, 1);
+    const int grid = (int)std::max<int64_t>(std::min<int64_t>(cells, p.groups), 1);
     float* const part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace) + kAttnTicketBytes);
     hipLaunchKernelGGL((paged_stream_kernel<DP, NQ, HG, 2, 4>), dim3(grid), dim3(256), C::kLds, stream, a, part,
-                       reinterpret_cast<unsigned int*>(workspace), grid, 2, C::KW == 1 ? 5 : 3);
+                       reinterpret_cast<unsigned int*>(workspace), grid, C::KW == 1 ? 5 : 3);
     return hipGetLastError();
 }
 
 template <int DP, int W>
-hipError_t launch_tiles(const PagedArgs& a, void* workspace, hipStream_t stream) {
+hipError_t launch_tiles(const PagedPlan& p, const PagedArgs& a, void* workspace, hipStream_t stream) {
     constexpr int kRows = 32 * W, kKeys = TileShape_<DP>::kKeys;
     constexpr int kLds = std::max(PagedTileShape<DP>::kLds, kRows * DP * 4);
     const int64_t units = ((int64_t)a.T * (a.Hq / a.H) / kRows + a.B) * a.H;
-    const int64_t steps = units * std::max<int64_t>((a.max_len + kKeys - 1) / kKeys, 1);
-    const int grid = (int)std::max<int64_t>(std::min<int64_t>(steps / 2, tile_groups(DP, W)), 1);
+    const int64_t cells = units * std::max<int64_t>(((a.max_len + kKeys - 1) / kKeys + 1) / kCell, 1);
+    const int grid = (int)std::max<int64_t>(std::min<int64_t>(cells, p.groups), 1);
     float* const part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace) + kAttnTicketBytes);
     unsigned int* const tickets = reinterpret_cast<unsigned int*>(workspace);
     if (a.per_tensor)
-        hipLaunchKernelGGL((paged_tile_kernel<DP, true, W>), dim3(grid), dim3(64 * W), kLds, stream, a, part, tickets, grid, 2, 3);
+        hipLaunchKernelGGL((paged_tile_kernel<DP, true, W>), dim3(grid), dim3(64 * W), kLds, stream, a, part, tickets, grid, 3);
     else
-        hipLaunchKernelGGL((paged_tile_kernel<DP, false, W>), dim3(grid), dim3(64 * W), kLds, stream, a, part, tickets, grid, 2, 3);
+        hipLaunchKernelGGL((paged_tile_kernel<DP, false, W>), dim3(grid), dim3(64 * W), kLds, stream, a, part, tickets, grid, 3);
     return hipGetLastError();
 }
 
 template <int DP>
 hipError_t launch_stream_rows(const PagedPlan& p, const PagedArgs& a, void* workspace, hipStream_t stream) {
     if constexpr (DP == 128)
-        if (p.tile_waves == 8) return launch_tiles<DP, 8>(a, workspace, stream);
-    if (p.tile_waves == 4) return launch_tiles<DP, 4>(a, workspace, stream);
+        if (p.tile_waves == 8) return launch_tiles<DP, 8>(p, a, workspace, stream);
+    if (p.tile_waves == 4) return launch_tiles<DP, 4>(p, a, workspace, stream);
     if (p.hg == 1)
-        return p.nq == 1 ? launch_stream<DP, 1, 1>(a, workspace, stream) : launch_stream<DP, 2, 1>(a, workspace, stream);
+        return p.nq == 1 ? launch_stream<DP, 1, 1>(p, a, workspace, stream) : launch_stream<DP, 2, 1>(p, a, workspace, stream);
     if (p.hg == 2)
-        return p.nq == 1 ? launch_stream<DP, 1, 2>(a, workspace, stream) : launch_stream<DP, 2, 2>(a, workspace, stream);
-    return launch_stream<DP, 1, 4>(a, workspace, stream);
+        return p.nq == 1 ? launch_stream<DP, 1, 2>(p, a, workspace, stream) : launch_stream<DP, 2, 2>(p, a, workspace, stream);
+    return launch_stream<DP, 1, 4>(p, a, workspace, stream);
 }
 
 }  // namespace
@@ -219,7 +218,7 @@ hipError_t launch_paged_attention(const PagedArgs& given, void* workspace, hipSt
         a.k_cache = a.v_cache = reinterpret_cast<const uint8_t*>(a.q);
         a.k_scale = a.v_scale = reinterpret_cast<const float*>(a.q);
     }
-    const PagedPlan p = plan_paged(a.T, a.B, a.Hq, a.H, a.D);
+    const PagedPlan p = plan_paged(a.T, a.B, a.Hq, a.H, a.D, a.max_len);
     if (p.dp == 64) return launch_stream_rows<64>(p, a, workspace, stream);
     if (p.dp == 128) return launch_stream_rows<128>(p, a, workspace, stream);
     if (p.dp == 256) return launch_stream_rows<256>(p, a, workspace, stream);

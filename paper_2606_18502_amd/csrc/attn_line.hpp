@@ -1,13 +1,15 @@
 // How the paged attention kernels share out their work, and join what is split.
 //
-// A unit is (sequence, ROWS rows of a KV head's group, HG KV heads); its cost is
-// its number of key steps, and `extra` for its beginning (queries, first loads,
-// what is stored at its end).  The units lie on one line in the order
-// sequence, heads, row tile (a head's tiles read the same keys), and the workgroups cut it into equal ranges, whatever
-// the sequences' lengths, which only the device knows.  A range covers whole units and parts of
-// at most two.  The parts of a unit are joined by the workgroup that stores the
-// last of them, found by a ticket per unit at the workgroup where the unit
-// starts; many parts in two rounds, the first over runs of parts.
+// A unit is (sequence, ROWS rows of a KV head's group, HG KV heads); its work is
+// its number of key steps.  The lengths are the device's, so the cut is made there.
+// Much work: the units lie on one line in the order sequence, heads, row tile (a head's tiles
+// read the same keys), each with its steps and `extra` more for its beginning and end,
+// and the workgroups cut the line into equal ranges, whatever the sequences' lengths: a
+// range covers whole units and parts of at most two.  Little work (fewer than kCell steps
+// for every workgroup): a unit is cut into cells of about kCell steps, one workgroup each; a
+// shorter one is not worth its join.
+// The parts of a unit are joined by the workgroup that stores the last of
+// them, found by a ticket; many parts in two rounds, the first over runs of parts.
 //
 // No fences: parts are stored and loaded with relaxed accesses at agent scope
 // (through to where all XCDs meet), a wave waits for the acknowledgement of its
@@ -21,6 +23,7 @@ namespace specfp8 {
 
 namespace {
 
+constexpr int kCell = 3;
 constexpr int kJoin = 16;                                    // parts that one workgroup joins at a time
 
 template <int THREADS>
@@ -33,46 +36,64 @@ struct LineShared {
 template <int THREADS, int ROWS, int STEP>
 struct Line {
     int64_t total, hi, pos, base;
-    int ng, wg, b, window_at, extra, nhg;
-    // the current segment: steps s_in .. s_in + count of a unit of `steps` whose first lies at u0
-    int64_t u0;
-    int first, n, L, steps, rt, hg, s_in, count;
+    int ng, wg, b, window_at, nhg;
+    int extra;                                               // < 0: cells
+    // the current segment: steps s_in .. s_in + count of a unit of `steps`, part `me` of `parts` from workgroup w0 on
+    int first, n, L, steps, rt, hg, s_in, count, w0, parts, me;
 
-    static __device__ __forceinline__ int64_t cost(const PagedArgs& a, int n, int L, int nhg, int extra) {
-        return (((int64_t)n * (a.Hq / a.H) + ROWS - 1) / ROWS) * nhg * (max((L + STEP - 1) / STEP, 1) + extra);
+    // what a unit takes of the line
+    static __device__ __forceinline__ int length(int steps, int extra) { return extra < 0 ? max((steps + 1) / kCell, 1) : steps + extra; }
+    static __device__ __forceinline__ int64_t units(const PagedArgs& a, int n, int nhg) {
+        return (((int64_t)n * (a.Hq / a.H) + ROWS - 1) / ROWS) * nhg;
     }
     static __device__ __forceinline__ int64_t cost_of(const PagedArgs& a, int b, int nhg, int extra) {
         int first, n;
         rows_of(a.cu_q, a.T, a.B, b, &first, &n);
-        return cost(a, n, min(max(a.kv_lens[b], 0), a.max_len), nhg, extra);
+        return units(a, n, nhg) * length(max((min(max(a.kv_lens[b], 0), a.max_len) + STEP - 1) / STEP, 1), extra);
     }
-
-    // This workgroup's range; false if it has none.  Called by all threads.
-    __device__ __forceinline__ bool begin(const PagedArgs& a, LineShared<THREADS>& sh, int heads, int groups,
-                                          int min_steps, int extra_) {
-        const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-        extra = extra_;
-        nhg = (a.H + heads - 1) / heads;
-        const int per = (a.B + THREADS - 1) / THREADS;
-        int64_t mine = 0;
-        for (int x = 0; x < per && tid * per + x < a.B; ++x) mine += cost_of(a, tid * per + x, nhg, extra);
+    static __device__ __forceinline__ int64_t sum_before(int64_t mine, int64_t* scan, int64_t* sum) {
+        const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
         int64_t upto = mine;
         for (int o = 1; o < 64; o <<= 1) {
             const int64_t v = __shfl_up(upto, o);
             if (lane >= o) upto += v;
         }
-        if (lane == 63) sh.scan[w] = upto;
+        if (lane == 63) scan[w] = upto;
         __syncthreads();
-        int64_t before = 0, sum = 0;
+        int64_t before = 0, all = 0;
         for (int x = 0; x < THREADS / 64; ++x) {
-            if (x < w) before += sh.scan[x];
-            sum += sh.scan[x];
+            if (x < w) before += scan[x];
+            all += scan[x];
         }
+        *sum = all;
+        return before + upto - mine;
+    }
+
+    // This workgroup's range; false if it has none.  Called by all threads.
+    __device__ __forceinline__ bool begin(const PagedArgs& a, LineShared<THREADS>& sh, int heads, int groups, int extra_) {
+        const int tid = threadIdx.x;
+        nhg = (a.H + heads - 1) / heads;
+        const int per = (a.B + THREADS - 1) / THREADS;
+        const auto sum_here = [&](int how) {
+            int64_t v = 0;
+            for (int x = 0; x < per && tid * per + x < a.B; ++x) v += cost_of(a, tid * per + x, nhg, how);
+            return v;
+        };
+        extra = -1;
+        int64_t mine = sum_here(-1), sum;
+        int64_t before = sum_before(mine, sh.scan, &sum);
         total = uniform(sum);
-        before += upto - mine;
-        const int64_t wanted = total / min_steps;            // (fewer steps are not worth a workgroup)
-        ng = uniform((int)(wanted < 1 ? 1 : (wanted < groups ? wanted : groups)));
-        if (total == 0 || (int)blockIdx.x >= ng) return false;
+        if (total == 0) return false;
+        if (total > groups) {
+            extra = extra_;
+            mine = sum_here(extra);
+            __syncthreads();
+            before = sum_before(mine, sh.scan, &sum);
+            total = uniform(sum);
+        }
+        // (in cells a workgroup's range is one; a line of more than `groups` cells has more steps than workgroups)
+        ng = uniform((int)min(total, (int64_t)groups));
+        if ((int)blockIdx.x >= ng) return false;
         // workgroups go round-robin over the XCDs: neighbours on the line share an XCD's L2
         const int xcd = blockIdx.x % 8;
         wg = xcd * (ng / 8) + min(xcd, ng % 8) + (int)(blockIdx.x / 8);
@@ -116,22 +137,37 @@ struct Line {
             n = uniform(sh.window[1][b - window_at]);
             L = uniform(sh.window[2][b - window_at]);
             steps = max((L + STEP - 1) / STEP, 1);
-            const int64_t c = cost(a, n, L, nhg, extra);
+            const int len = length(steps, extra);
+            const int64_t c = units(a, n, nhg) * len;
             if (pos >= base + c) {
                 base += c;
                 ++b;
                 continue;
             }
-            const int unit = uniform((int)((pos - base) / (steps + extra)));
+            const int unit = uniform((int)((pos - base) / len));
             const int tiles = (int)(((int64_t)n * (a.Hq / a.H) + ROWS - 1) / ROWS);
             hg = unit / tiles;
             rt = unit - hg * tiles;
-            u0 = base + (int64_t)unit * (steps + extra) + extra;
+            const int64_t at = base + (int64_t)unit * len;   // the unit's place
+            if (extra < 0) {
+                w0 = (int)at;
+                parts = len;
+                me = (int)(pos - at);
+                s_in = (int)((int64_t)steps * me / len);
+                count = (int)((int64_t)steps * (me + 1) / len) - s_in;
+                ++pos;
+                return true;
+            }
+            const int64_t u0 = at + extra;                   // where its steps lie
             s_in = (int)max(pos - u0, (int64_t)0);
             const int s_out = (int)min(hi - u0, (int64_t)steps);
             pos = u0 + max(s_out, 0);
             count = s_out - s_in;
-            return count > 0;                                // (0: a unit's beginning alone lies at the range's end)
+            if (count <= 0) return false;                    // (its beginning alone lies at the range's end)
+            w0 = workgroup_of(u0);
+            parts = workgroup_of(u0 + steps - 1) - w0 + 1;
+            me = wg - w0;
+            return true;
         }
         return false;
     }
@@ -147,14 +183,11 @@ struct Parts {
                                                              // row's reference and sum of p, and those of a run
     float* part;
     unsigned int* tickets;
-    int groups, w0, parts, run, me;
+    int groups, w0, parts, me, run;
 
     __device__ __forceinline__ Parts(const Line<THREADS, ROWS, STEP>& l, float* part_, unsigned int* tickets_, int groups_)
-        : part(part_), tickets(tickets_), groups(groups_) {
-        w0 = l.workgroup_of(l.u0);
-        parts = l.workgroup_of(l.u0 + l.steps - 1) - w0 + 1;
+        : part(part_), tickets(tickets_), groups(groups_), w0(l.w0), parts(l.parts), me(l.me) {
         run = parts <= 3 * kJoin / 2 ? parts : kJoin;
-        me = l.wg - w0;
     }
     // (a workgroup has a part of at most one unit that starts in it, and of one that started before)
     __device__ __forceinline__ int slot(int x) const { return 2 * (w0 + x) + (x == 0 ? 1 : 0); }

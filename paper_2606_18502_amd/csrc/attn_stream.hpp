@@ -68,7 +68,7 @@ struct StreamShape {
 
 template <int DP, int NQ, int HG, int S, int W>
 __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel(PagedArgs a, float* part, unsigned int* tickets,
-                                                                      int groups, int min_steps, int extra) {
+                                                                      int groups, int extra) {
     using C = StreamShape<DP, NQ, HG, S, W>;
     constexpr int NB = C::kBlocks, KS = DP / 64;
     // (sized at the launch: with the size in its view the compiler counts on one workgroup per CU, and then keeps the
@@ -80,7 +80,7 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
     const int q16 = lane & 15, qd = lane >> 4;
 
     Line<64 * W, C::kRows, C::kStep> line;
-    if (!line.begin(a, sh, HG, groups, min_steps, extra)) return;
+    if (!line.begin(a, sh, HG, groups, extra)) return;
 
     // ---- this wave's corner of LDS
     const int hw = w % HG, kw = w / HG;

@@ -453,7 +453,7 @@ struct PagedTileShape {
 
 template <int DP, bool PT, int W>
 __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_tile_kernel(PagedArgs a, float* part, unsigned int* tickets,
-                                                                            int groups, int min_steps, int extra) {
+                                                                            int groups, int extra) {
     using C = TileShape_<DP>;
     constexpr int kThreads = 64 * W, kRows = 32 * W;
     using PartsT = Parts<kThreads, kRows, C::kKeys, 1, DP>;
@@ -462,14 +462,16 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_tile_kernel(P
     const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), h = lane >> 5, l32 = lane & 31;
     const int G = a.Hq / a.H;
     Line<kThreads, kRows, C::kKeys> line;
-    if (!line.begin(a, sh, 1, groups, min_steps, extra)) return;
+    if (!line.begin(a, sh, 1, groups, extra)) return;
 
     const uint32_t smem = uniform((int)lds_at(tile_smem));
     float* const scales = reinterpret_cast<float*>(tile_smem + PagedTileShape<DP>::kScales);      // [2][128]
     uint64_t* const masks = reinterpret_cast<uint64_t*>(scales + 256);                            // [2]
     // loads: 16 codes of key tid/kChunks + x kKeys16; table entries of those keys, and of the key whose scale this is
     constexpr int kChunks = DP / 16, kPer = kThreads / kChunks, NL = 64 / kPer;
-    const int ld_key = tid / kChunks, ld_chunk = tid % kChunks, sc_key = tid & 63;
+    const int ld_row = tid / kChunks, ld_chunk = tid % kChunks, sc_key = tid & 63;
+    // (rows 1 and 2 of each four change places: an LDS cycle serves lanes l and l + 16, whose chunks then differ)
+    const int ld_key = DP == 128 ? (ld_row & ~3) | ((ld_row & 1) << 1) | ((ld_row >> 1) & 1) : ld_row;
     const int src_chunk = ld_chunk * 16 < a.D ? ld_chunk * 16 : 0;             // (past the head's end: any; queries are 0)
     // (a page has less than 4 GiB of codes)
     const int bs = a.block_size, step_q = C::kKeys / bs, step_r = C::kKeys % bs;
@@ -612,9 +614,10 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_tile_kernel(P
                     __syncthreads();
                 }
             }
-            if (k0 <= wave_last)
-                attend_tile<DP, !PT>(st, q, kt, kt + C::kTile, sees(k0) & mask,
-                                     mask == ~0ull && k0 + C::kKeys - 1 <= wave_all, c2, sc, sc + 64);
+            if (k0 <= wave_last) {
+                const bool full = mask == ~0ull && k0 + C::kKeys - 1 <= wave_all;
+                attend_tile<DP, !PT>(st, q, kt, kt + C::kTile, full ? 0 : sees(k0) & mask, full, c2, sc, sc + 64);
+            }
             if (t + 1 < count) write(t + 1);
             __syncthreads();
         }

@@ -187,25 +187,32 @@ AcceptPlan plan_accept(int64_t B, int64_t k, int64_t V) {
     return p;
 }
 
-PagedPlan plan_paged(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D) {
-    PagedPlan p{0, 0, 1, 0, kAttnTicketBytes};
+PagedPlan plan_paged(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t max_len) {
+    PagedPlan p{0, 0, 1, 0, 0, kAttnTicketBytes};
     if (D % 16 != 0) return p;
     p.dp = D <= 64 ? 64 : (D <= 128 ? 128 : 256);
     const int64_t rows = (T + B - 1) / B * (Hq / H);       // of an average sequence and one KV head
-    static const int64_t lim = getenv("AR") ? atoi(getenv("AR")) : 32, lim8 = getenv("A8") ? atoi(getenv("A8")) : 128;
+    static const int64_t lim = getenv("AR") ? atoi(getenv("AR")) : 128, lim8 = getenv("A8") ? atoi(getenv("A8")) : 128;
     if (rows > lim) {
         p.tile_waves = p.dp == 128 && rows > lim8 ? 8 : 4;
-        p.bytes += (size_t)tile_groups(p.dp, p.tile_waves) * 2 * 32 * p.tile_waves * (p.dp + 4) * sizeof(float);
+        p.groups = p.dp == 256 || p.tile_waves == 8 ? 256 : 512;
+        p.bytes += (size_t)p.groups * 2 * 32 * p.tile_waves * (p.dp + 4) * sizeof(float);
         return p;
     }
     p.nq = rows <= 16 ? 1 : 2;
-    p.hg = H == 1 ? 1 : (H == 2 || p.nq == 2 ? 2 : 4);
-    p.bytes += (size_t)kAttnGroups * 2 * p.hg * p.nq * 16 * (p.dp + 4) * sizeof(float);
+    p.groups = rows > 32 ? 512 : 256;
+    p.hg = H == 1 || rows > 32 ? 1 : (H == 2 || p.nq == 2 ? 2 : 4);
+    static const int ag = getenv("AG") ? atoi(getenv("AG")) : 0, ah = getenv("AH") ? atoi(getenv("AH")) : 0;
+    if (ag) p.groups = ag;
+    if (ah) p.hg = ah;
+    // a short line: one head a workgroup
+    if (B * ((H + p.hg - 1) / p.hg) * ((max_len * p.hg + 127) / 128) / 3 < p.groups) p.hg = 1;
+    p.bytes += (size_t)512 * 2 * 4 * 32 * (p.dp + 4) * sizeof(float);
     return p;
 }
 
 size_t paged_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D) {
-    return plan_paged(T, B, Hq, H, D).bytes;
+    return plan_paged(T, B, Hq, H, D, 2147483647).bytes;
 }
 
 }  // namespace specfp8

@@ -97,15 +97,13 @@ constexpr int64_t kAcceptChunk = (int64_t)kAcceptThreads * kAcceptPerThread;   /
 
 // ---- paged attention ----------------------------------------------------------
 constexpr size_t kAttnTicketBytes = 16384;   // at the start of the workspace, zero between calls
-constexpr int kAttnGroups = 256;             // workgroups of a stream over the cache, one ticket each
 
 // A call's kernel: D padded to dp (64, 128, 256; 0: the row kernel, for heads that are no multiple
 // of 16), 16*nq rows per unit, hg KV heads per workgroup.
 struct PagedPlan {
-    int dp, nq, hg, tile_waves;
+    int dp, nq, hg, tile_waves, groups;
     size_t bytes;          // of workspace: the tickets, then two parts per workgroup
 };
-constexpr int tile_groups(int dp, int waves) { return dp == 256 || waves == 8 ? 256 : 512; }   // two per CU where they fit
-PagedPlan plan_paged(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D);
+PagedPlan plan_paged(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t max_len);
 
 }  // namespace specfp8
