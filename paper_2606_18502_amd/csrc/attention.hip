@@ -174,7 +174,7 @@ hipError_t launch_stream(const PagedPlan& p, const PagedArgs& a, void* workspace
     using C = StreamShape<DP, NQ, HG, 2, 4>;
     // The lengths are the device's: never more workgroups than there are cells where every sequence fills its table.
     const int64_t units = ((int64_t)a.T * (a.Hq / a.H) / C::kRows + a.B) * ((a.H + HG - 1) / HG);
-    const int64_t cells = units * std::max<int64_t>(((a.max_len + C::kStep - 1) / C::kStep + 1) / kCell, 1);
+    const int64_t cells = units * std::max<int64_t>(((a.max_len + C::kStep - 1) / C::kStep + 1) / kStreamCell, 1);
     const int grid = (int)std::max<int64_t>(std::min<int64_t>(cells, p.groups), 1);
     float* const part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace) + kAttnTicketBytes);
     hipLaunchKernelGGL((paged_stream_kernel<DP, NQ, HG, 2, 4>), dim3(grid), dim3(256), C::kLds, stream, a, part,
@@ -187,7 +187,7 @@ hipError_t launch_tiles(const PagedPlan& p, const PagedArgs& a, void* workspace,
     constexpr int kRows = 32 * W, kKeys = TileShape_<DP>::kKeys;
     constexpr int kLds = std::max(PagedTileShape<DP>::kLds, kRows * DP * 4);
     const int64_t units = ((int64_t)a.T * (a.Hq / a.H) / kRows + a.B) * a.H;
-    const int64_t cells = units * std::max<int64_t>(((a.max_len + kKeys - 1) / kKeys + 1) / kCell, 1);
+    const int64_t cells = units * std::max<int64_t>(((a.max_len + kKeys - 1) / kKeys + 1) / kTileCell, 1);
     const int grid = (int)std::max<int64_t>(std::min<int64_t>(cells, p.groups), 1);
     float* const part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace) + kAttnTicketBytes);
     unsigned int* const tickets = reinterpret_cast<unsigned int*>(workspace);

@@ -5,8 +5,8 @@
 // Much work: the units lie on one line in the order sequence, heads, row tile (a head's tiles
 // read the same keys), each with its steps and `extra` more for its beginning and end,
 // and the workgroups cut the line into equal ranges, whatever the sequences' lengths: a
-// range covers whole units and parts of at most two.  Little work (fewer than kCell steps
-// for every workgroup): a unit is cut into cells of about kCell steps, one workgroup each; a
+// range covers whole units and parts of at most two.  Little work (fewer than CELL steps
+// for every workgroup): a unit is cut into cells of about CELL steps, one workgroup each; a
 // shorter one is not worth its join.
 // The parts of a unit are joined by the workgroup that stores the last of
 // them, found by a ticket; many parts in two rounds, the first over runs of parts.
@@ -23,7 +23,6 @@ namespace specfp8 {
 
 namespace {
 
-constexpr int kCell = 3;
 constexpr int kJoin = 16;                                    // parts that one workgroup joins at a time
 
 template <int THREADS>
@@ -33,7 +32,7 @@ struct LineShared {
     int is_last;
 };
 
-template <int THREADS, int ROWS, int STEP>
+template <int THREADS, int ROWS, int STEP, int CELL>
 struct Line {
     int64_t total, hi, pos, base;
     int ng, wg, b, window_at, nhg;
@@ -42,7 +41,7 @@ struct Line {
     int first, n, L, steps, rt, hg, s_in, count, w0, parts, me;
 
     // what a unit takes of the line
-    static __device__ __forceinline__ int length(int steps, int extra) { return extra < 0 ? max((steps + 1) / kCell, 1) : steps + extra; }
+    static __device__ __forceinline__ int length(int steps, int extra) { return extra < 0 ? max((steps + 1) / CELL, 1) : steps + extra; }
     static __device__ __forceinline__ int64_t units(const PagedArgs& a, int n, int nhg) {
         return (((int64_t)n * (a.Hq / a.H) + ROWS - 1) / ROWS) * nhg;
     }
@@ -177,7 +176,7 @@ struct Line {
 };
 
 // The parts of a line's current unit.
-template <int THREADS, int ROWS, int STEP, int HG, int DP>
+template <int THREADS, int ROWS, int HG, int DP, class LINE>
 struct Parts {
     static constexpr int kPart = HG * ROWS * (DP + 4);       // floats: HG heads of ROWS rows of DP sums, then each
                                                              // row's reference and sum of p, and those of a run
@@ -185,7 +184,7 @@ struct Parts {
     unsigned int* tickets;
     int groups, w0, parts, me, run;
 
-    __device__ __forceinline__ Parts(const Line<THREADS, ROWS, STEP>& l, float* part_, unsigned int* tickets_, int groups_)
+    __device__ __forceinline__ Parts(const LINE& l, float* part_, unsigned int* tickets_, int groups_)
         : part(part_), tickets(tickets_), groups(groups_), w0(l.w0), parts(l.parts), me(l.me) {
         run = parts <= 3 * kJoin / 2 ? parts : kJoin;
     }
@@ -213,7 +212,7 @@ struct Parts {
 
     // Parts x0, x0 + step, .. below x1, in the line's order whoever came last, to the output or to the place of
     // the first.  A thread takes four channels of K rows; Z parts of them are in flight at a time.
-    __device__ __forceinline__ void join(const PagedArgs& a, const Line<THREADS, ROWS, STEP>& l, int x0, int x1, int step,
+    __device__ __forceinline__ void join(const PagedArgs& a, const LINE& l, int x0, int x1, int step,
                                          int round, bool output) const {
         constexpr int K = 2, Z = 8;
         const int G = a.Hq / a.H, R = l.n * G;
@@ -284,7 +283,7 @@ struct Parts {
     }
 
     // After this workgroup's part has been stored: the joins that fall to it.  Called by all threads.
-    __device__ __forceinline__ void finish(const PagedArgs& a, const Line<THREADS, ROWS, STEP>& l, LineShared<THREADS>& sh) const {
+    __device__ __forceinline__ void finish(const PagedArgs& a, const LINE& l, LineShared<THREADS>& sh) const {
         const int r0 = me / run * run, runs = (parts + run - 1) / run;
         if (last_of(tickets + slot(r0), min(run, parts - r0), sh)) {
             join(a, l, r0, min(r0 + run, parts), 1, 0, runs == 1);

@@ -48,6 +48,8 @@ __device__ __forceinline__ int v_swizzle(int r) {
     else return (r & 7) | (((r >> 4) & 1) << 3);
 }
 
+constexpr int kStreamCell = 3;                               // steps that are worth a join (1, 2, 4: slower on short lines)
+
 template <int DP, int NQ, int HG, int S, int W>
 struct StreamShape {
     static constexpr int KW = W / HG;             // waves that share a head
@@ -79,7 +81,7 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
     const int G = a.Hq / a.H;
     const int q16 = lane & 15, qd = lane >> 4;
 
-    Line<64 * W, C::kRows, C::kStep> line;
+    Line<64 * W, C::kRows, C::kStep, kStreamCell> line;
     if (!line.begin(a, sh, HG, groups, extra)) return;
 
     // ---- this wave's corner of LDS
@@ -94,6 +96,9 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
     const int chunks = a.D / 16;
     const int bs = a.block_size, step_q = C::kStep / bs, step_r = C::kStep % bs;
     const int last_block = max(a.max_len / bs - 1, 0);
+    // (as a scalar of its own: a loop that reads one field of the arguments keeps, or reloads, eight)
+    const uint32_t num_blocks = uniform(a.num_blocks), head_size = uniform(a.D);
+    const int heads = uniform(a.H), per_tensor = uniform(a.per_tensor);
     const float* const scales = lane < 32 ? a.k_scale : a.v_scale;
     const uint32_t page_rows = bs * a.H, page_bytes = page_rows * a.D;          // (a page has less than 4 GiB of codes)
     const float c2 = a.scale * 1.4426950408889634f;
@@ -158,11 +163,11 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
             int next_key = first_key;
             const auto prepare = [&](int t) -> uint32_t {            // byte offsets and scales of tile t; which keys there are
                 const int page = (int)tab[(t % S) * 64 + lane];
-                const bool there = next_key + key < L && page >= 0 && page < a.num_blocks;
-                const uint32_t pg = there ? page : 0, in = (there ? off_p : 0) * a.H + head;
+                const bool there = (next_key + key < L) & ((uint32_t)page < num_blocks);
+                const uint32_t pg = there ? page : 0, in = (there ? off_p : 0) * heads + head;
                 const uint64_t row = (uint64_t)pg * page_rows + in;
-                if (lane < 32) offs[key] = (int64_t)((uint64_t)pg * page_bytes + in * (uint32_t)a.D);
-                load_lds4(scales + (a.per_tensor ? 0 : row), ring_at + (t % S) * C::kStage + 2 * C::kTile);
+                if (lane < 32) offs[key] = (int64_t)((uint64_t)pg * page_bytes + in * head_size);
+                load_lds4(scales + (per_tensor ? 0 : row), ring_at + (t % S) * C::kStage + 2 * C::kTile);
                 off_p += step_r;
                 if (off_p >= bs) off_p -= bs;
                 next_key += C::kStep;
@@ -456,7 +461,7 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
                 for (int x = 0; x < NQ; ++x) store_rows(x, head, l[x], o[x]);
             }
         } else {
-            const Parts<64 * W, C::kRows, C::kStep, HG, DP> parts(line, part, tickets, groups);
+            const Parts<64 * W, C::kRows, HG, DP, decltype(line)> parts(line, part, tickets, groups);
             if (active && kw == 0) {
                 float* const to = parts.sums(parts.me) + hw * C::kRows * DP;
 #pragma unroll

@@ -108,12 +108,15 @@ __device__ __forceinline__ void attend_tile(RowState<DP>& st, const bf16x8_t (&q
             s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[ks], s[kb], 0, 0, 0);
         }
     }
+    const bool fresh = st.m == kLowest;                      // (no reference yet)
     if constexpr (SCALED) {
+        const float ref = fresh ? 0.0f : st.m;
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
             const f32x4_t f = *reinterpret_cast<const f32x4_t*>(k_scales + 8 * x + 4 * h);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[x >> 2][4 * (x & 3) + e] *= f[e];
+            for (int e = 0; e < 4; ++e)                      // over the reference already: one instruction, not two
+                s[x >> 2][4 * (x & 3) + e] = fmaf(s[x >> 2][4 * (x & 3) + e], f[e], -ref);
         }
     }
     if (!full) {
@@ -130,10 +133,22 @@ __device__ __forceinline__ void attend_tile(RowState<DP>& st, const bf16x8_t (&q
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, s[1][i]);
     if constexpr (!SCALED) top *= c2;
-    if (__ballot(top > st.m + kLazy)) {
-        const float mx = fmaxf(st.m, max_halves(top));
-        const float down = exp2_hw(st.m - mx);
-        st.m = mx;
+    if (SCALED ? __ballot(top > kLazy || (fresh && top > kLowest)) : __ballot(top > st.m + kLazy)) {
+        float down;
+        if constexpr (SCALED) {
+            const float mx = max_halves(top);
+            const float up = fresh ? (mx > kLowest ? mx : 0.0f) : fmaxf(0.0f, mx);
+            down = fresh ? 1.0f : exp2_hw(-up);
+            st.m = fresh ? (mx > kLowest ? mx : kLowest) : st.m + up;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[kb][i] -= up;
+        } else {
+            const float mx = fmaxf(st.m, max_halves(top));
+            down = exp2_hw(st.m - mx);
+            st.m = mx;
+        }
         st.l *= down;
 #pragma unroll
         for (int d = 0; d < C::DB; ++d) st.o[d] *= down;
@@ -149,8 +164,8 @@ __device__ __forceinline__ void attend_tile(RowState<DP>& st, const bf16x8_t (&q
             const int i = 8 * (u & 1) + 2 * e;
             float a, b;
             if constexpr (SCALED) {
-                a = exp2_hw(s[u >> 1][i] - st.m);
-                b = exp2_hw(s[u >> 1][i + 1] - st.m);
+                a = exp2_hw(s[u >> 1][i]);
+                b = exp2_hw(s[u >> 1][i + 1]);
             } else {
                 a = exp2_hw(fmaf(s[u >> 1][i], c2, -st.m));
                 b = exp2_hw(fmaf(s[u >> 1][i + 1], c2, -st.m));
@@ -445,6 +460,8 @@ struct RowBox {
     }
 };
 
+constexpr int kTileCell = 8;                                 // steps that are worth a join of a whole tile's rows
+
 template <int DP>
 struct PagedTileShape {
     static constexpr int kScales = 4 * TileShape_<DP>::kTile;                  // two tiles' 64 + 64 scales and masks
@@ -456,12 +473,11 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_tile_kernel(P
                                                                             int groups, int extra) {
     using C = TileShape_<DP>;
     constexpr int kThreads = 64 * W, kRows = 32 * W;
-    using PartsT = Parts<kThreads, kRows, C::kKeys, 1, DP>;
     extern __shared__ __attribute__((aligned(1024))) uint8_t tile_smem[];
     __shared__ LineShared<kThreads> sh;
     const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), h = lane >> 5, l32 = lane & 31;
     const int G = a.Hq / a.H;
-    Line<kThreads, kRows, C::kKeys> line;
+    Line<kThreads, kRows, C::kKeys, kTileCell> line;
     if (!line.begin(a, sh, 1, groups, extra)) return;
 
     const uint32_t smem = uniform((int)lds_at(tile_smem));
@@ -477,6 +493,10 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_tile_kernel(P
     const int bs = a.block_size, step_q = C::kKeys / bs, step_r = C::kKeys % bs;
     const uint32_t row_bytes = a.H * a.D, page_bytes = bs * row_bytes, page_rows = bs * a.H;
     const int last_block = max(a.max_len / bs - 1, 0);
+    // (as scalars of their own: a loop that reads one field of the arguments keeps, or reloads, eight)
+    const uint32_t num_blocks = uniform(a.num_blocks);
+    const int heads = uniform(a.H);
+    const float* const scale_from = tid & 64 ? a.v_scale : a.k_scale;
     const float c2 = a.scale * 1.4426950408889634f * (PT ? a.k_scale[0] : 1.0f);
 
     while (line.next(a, sh)) {
@@ -504,10 +524,11 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_tile_kernel(P
         const int wave_last = row0 + 32 * w >= R ? -1 : a.tree ? L - 1 : L - n + uniform(first_of(min(row0 + 32 * w + 31, R - 1)));
         const int last = a.tree ? L - 1 : L - n + uniform(first_of(min(row0 + kRows, R) - 1));
         const int count = min(line.count, (last >> 6) + 1 - line.s_in);        // (tiles that some row sees)
+        const int is_tree = uniform(a.tree ? 1 : 0), node0 = uniform(L - a.N);
         const auto sees = [&](int k0) -> uint64_t {
             uint64_t m = first_keys(lim + 1 - k0);
-            if (a.tree) {
-                const int f = k0 - (L - a.N);                                  // node number of the tile's first key
+            if (is_tree) {
+                const int f = k0 - node0;                                       // node number of the tile's first key
                 if (f >= 0) m &= f < 64 ? nodes >> f : 0;
                 else if (f > -64) m &= nodes << -f | ((1ull << -f) - 1);
             }
@@ -537,6 +558,7 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_tile_kernel(P
                 }
             }
         };
+        const uint32_t head_bytes = uniform(head * a.D);
         const uint8_t *const k_from = a.k_cache + src_chunk, *const v_from = a.v_cache + src_chunk;
         u32x4_t kc[NL], vc[NL];
         float scale = 0.0f;
@@ -546,18 +568,18 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_tile_kernel(P
 #pragma unroll
             for (int x = 0; x <= NL; ++x) {
                 const int k = code_key0 + (x < NL ? ld_key + x * kPer : sc_key);
-                const bool ok = k < L && page[x] >= 0 && page[x] < a.num_blocks;
+                const bool ok = (k < L) & ((uint32_t)page[x] < num_blocks);
                 const uint32_t pg = ok ? page[x] : 0, in = ok ? in_page[x] : 0;           // (not there: some row)
                 if (x < NL) {
-                    const uint64_t r = (uint64_t)pg * page_bytes + (in * row_bytes + head * a.D);
+                    const uint64_t r = (uint64_t)pg * page_bytes + (in * row_bytes + head_bytes);
                     kc[x] = *reinterpret_cast<const u32x4_t*>(k_from + r);
                     vc[x] = *reinterpret_cast<const u32x4_t*>(v_from + r);
                 } else {
-                    const uint64_t r = (uint64_t)pg * page_rows + (in * a.H + head);
+                    const uint64_t r = (uint64_t)pg * page_rows + (in * heads + head);
                     present = __ballot(ok);
                     if constexpr (!PT) {
                         scale_there = ok;
-                        scale = (tid & 64 ? a.v_scale : a.k_scale)[r];
+                        scale = scale_from[r];
                     }
                 }
             }
@@ -626,7 +648,7 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_tile_kernel(P
         if (line.whole()) {
             if (there) store_rows(st, a.out + (int64_t)(first + i) * a.ld_out + (int64_t)(head * G + g) * a.D, a.D, v_scale);
         } else {
-            const PartsT parts(line, part, tickets, groups);
+            const Parts<kThreads, kRows, 1, DP, decltype(line)> parts(line, part, tickets, groups);
             f32x4_t* const box = reinterpret_cast<f32x4_t*>(tile_smem + w * 32 * DP * 4);
 #pragma unroll
             for (int d = 0; d < C::DB; ++d)
