@@ -476,7 +476,8 @@ spec_status spec_tree_attention_mask(const int32_t* parents, int64_t B, int64_t 
  *            spec_fp8_kv_cache_write; all read here.
  * k, v       bf16 [T, ld_k] / [T, ld_v]; head h at columns [h*D, (h+1)*D), the other
  *            columns keep their contents.
- * Requirements: those of spec_fp8_kv_cache_write.  num_slots == 0 reads zeros.
+ * Requirements: those of spec_fp8_kv_cache_write, and H*D < 2^32 (SPEC_ERR_UNSUPPORTED).
+ * num_slots == 0 reads zeros.
  */
 spec_status spec_fp8_kv_cache_read(const uint8_t* k_cache, const uint8_t* v_cache, const float* k_scale,
                                    const float* v_scale, spec_scale_mode mode, const int64_t* slot_mapping, int64_t T,
@@ -506,8 +507,8 @@ spec_status spec_fp8_kv_cache_read(const uint8_t* k_cache, const uint8_t* v_cach
  * over the tokens seen (m_i: a reference within 2^8 of the largest s_ij); a row that sees none, or only scores
  * of -inf, is zeros.  What a row does not see has no influence on it, NaN codes and scales
  * included.  Products of q and codes are exact; they are summed, and the sums
- * of p and p*v accumulated, in fp32; p_ij * sv_j is rounded to bf16 (to nearest)
- * for the second product.
+ * of p and p*v accumulated, in fp32; p_ij * sv_j (or p_ij alone, where one
+ * scale holds for the tensor) is rounded to bf16 (to nearest) for the second product.
  *
  * q        bf16 [T, ld_q], head h at columns [h*D, (h+1)*D).  The rows of sequence b are
  *          cu_q[b] .. cu_q[b+1]-1, or with cu_q NULL T/B rows each (T % B == 0,
@@ -557,9 +558,9 @@ spec_status spec_fp8_paged_attention(const void* q, int64_t ld_q, const uint8_t*
  *    cu_seqlens[B]) are neither read nor written.
  * out bf16 [T, ld_out]; may not overlap the inputs.
  * Requirements: T, B >= 0 (0: no-op), Hq, H, D > 0, Hq % H == 0, ld_q, ld_out >= Hq*D, ld_k,
- * ld_v >= H*D (SPEC_ERR_SHAPE); D % 8 == 0, D <= 256, Hq <= 65535, T*Hq and B < 2^31 (SPEC_ERR_UNSUPPORTED);
- * all tensors 16-byte aligned with strides that are multiples of 8, cu_seqlens 4-byte aligned
- * (SPEC_ERR_ALIGN); scale finite and > 0 (SPEC_ERR_VALUE).  No workspace.
+ * ld_v >= H*D (SPEC_ERR_SHAPE); D % 8 == 0, D <= 256, Hq <= 65535, T*Hq and B < 2^31,
+ * (T*Hq/H/128 + B)*H < 2^24 (SPEC_ERR_UNSUPPORTED); all tensors 16-byte aligned with strides
+ * that are multiples of 8, cu_seqlens 4-byte aligned (SPEC_ERR_ALIGN); scale finite and > 0 (SPEC_ERR_VALUE).  No workspace.
  */
 spec_status spec_prompt_attention_bf16(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v,
                                        int64_t ld_v, const int32_t* cu_seqlens, int64_t T, int64_t B, int64_t Hq,

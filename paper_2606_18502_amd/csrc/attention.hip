@@ -73,64 +73,38 @@ __device__ __forceinline__ int seq_of(const int32_t* cu, int T, int B, int t) {
     return lo;
 }
 
-// One wave per (row, query head): lanes over 64 keys for the scores, over D for the sums.
-template <bool PAGED>
-__global__ __launch_bounds__(kRowThreads) void attention_row_kernel(PagedArgs a, PromptArgs r) {
-    __shared__ float qs[kRowWaves][kMaxD];
-    const int w = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-    const int T = PAGED ? a.T : r.T, Hq = PAGED ? a.Hq : r.Hq, H = PAGED ? a.H : r.H, D = PAGED ? a.D : r.D;
-    const int64_t item = (int64_t)blockIdx.x * kRowWaves + w;
-    const int t = (int)(item / Hq), head = (int)(item % Hq), kvh = head / (Hq / H);
-    const bool row = t < T;
-    const int b = row ? (PAGED ? seq_of(a.cu_q, T, a.B, t) : seq_of(r.cu, T, r.B, t)) : -1;
-    const uint16_t* q = (PAGED ? a.q + (int64_t)t * a.ld_q : r.q + (int64_t)t * r.ld_q) + (int64_t)head * D;
-    if (b >= 0)
-        for (int d = lane; d < D; d += kWave) qs[w][d] = bf16_to_f32(q[d]);
-    __syncthreads();
-    if (b < 0) return;
-    int first, n, L;
-    rows_of(PAGED ? a.cu_q : r.cu, T, PAGED ? a.B : r.B, b, &first, &n);
-    L = PAGED ? min(max(a.kv_lens[b], 0), a.max_len) : n;
-    const int i = t - first, last = PAGED && a.tree ? L - 1 : L - n + i;
-    const uint64_t mask = PAGED && a.tree && i > 0 ? a.tree[(int64_t)b * a.N + i - 1] : 0;
+// Heads whose rows are not whole 16-byte pieces of codes (D % 16 == 8): one wave per (row, query head),
+// lanes over 64 keys for the scores, then over D for the sums.  All fp32 on the vector units, 64 keys a step,
+// the running maximum and sum of the softmax; bounded by its dot products (every wave reads its keys again).
+// ROW_FIGURES
+__device__ __forceinline__ void attend_row(const PagedArgs& a, const float* qs, int b, int t, int head) {
+    const int lane = threadIdx.x % kWave, D = a.D, H = a.H, kvh = head / (a.Hq / H);
+    int first, n;
+    rows_of(a.cu_q, a.T, a.B, b, &first, &n);
+    const int L = min(max(a.kv_lens[b], 0), a.max_len), i = t - first, last = a.tree ? L - 1 : L - n + i;
+    const uint64_t mask = a.tree && i > 0 ? a.tree[(int64_t)b * a.N + i - 1] : 0;
     float m = -INFINITY, sum = 0.0f, o[kMaxD / kWave] = {};
     for (int j0 = 0; j0 <= last; j0 += kWave) {
         const int j = j0 + lane;
         bool seen = j <= last;
-        int64_t at = 0;
-        if constexpr (PAGED) {
-            if (a.tree && seen && j >= L - a.N) seen = (mask >> (j - (L - a.N))) & 1;
-            int page = -1;
-            if (seen) page = a.tables[(int64_t)b * a.ld_tables + j / a.block_size];
-            seen = seen && page >= 0 && page < a.num_blocks;
-            at = seen ? ((int64_t)page * a.block_size + j % a.block_size) * H + kvh : 0;
-        } else {
-            at = (int64_t)(first + (seen ? j : 0));
-        }
-        float s = 0.0f, sv = 1.0f;
+        if (a.tree && seen && j >= L - a.N) seen = (mask >> (j - (L - a.N))) & 1;
+        int page = -1;
+        if (seen) page = a.tables[(int64_t)b * a.ld_tables + j / a.block_size];
+        seen = seen && page >= 0 && page < a.num_blocks;
+        const int64_t at = seen ? ((int64_t)page * a.block_size + j % a.block_size) * H + kvh : 0;
+        float s = -INFINITY, sv = 1.0f;
         if (seen) {
+            s = 0.0f;
             for (int d = 0; d < D; d += 8) {
-                if constexpr (PAGED) {
-                    const uint2 c = *reinterpret_cast<const uint2*>(a.k_cache + at * D + d);
+                const uint2 c = *reinterpret_cast<const uint2*>(a.k_cache + at * D + d);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const uint32_t x = (e < 4 ? c.x : c.y) >> (8 * (e & 3));
-                        s = fmaf(qs[w][d + e], __builtin_amdgcn_cvt_f32_fp8((int)x, 0), s);
-                    }
-                } else {
-                    float k[8];
-                    unpack8(*reinterpret_cast<const uint4*>(r.k + at * r.ld_k + (int64_t)kvh * D + d), k);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) s = fmaf(qs[w][d + e], k[e], s);
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t x = (e < 4 ? c.x : c.y) >> (8 * (e & 3));
+                    s = fmaf(qs[d + e], __builtin_amdgcn_cvt_f32_fp8((int)x, 0), s);
                 }
             }
-            if constexpr (PAGED) {
-                s *= a.per_tensor ? a.k_scale[0] : a.k_scale[at];
-                sv = a.per_tensor ? a.v_scale[0] : a.v_scale[at];
-            }
-            s *= (PAGED ? a.scale : r.scale) * 1.44269504f;
-        } else {
-            s = -INFINITY;
+            s *= (a.per_tensor ? a.k_scale[0] : a.k_scale[at]) * (a.scale * 1.44269504f);
+            sv = a.per_tensor ? a.v_scale[0] : a.v_scale[at];
         }
         const float top = fmaxf(m, wave_max(s));
         const float ref = top == -INFINITY ? 0.0f : top;
@@ -148,16 +122,11 @@ __global__ __launch_bounds__(kRowThreads) void attention_row_kernel(PagedArgs a,
 #pragma unroll
             for (int x = 0; x < kMaxD / kWave; ++x) {
                 const int d = lane + kWave * x;
-                if (d < D) {
-                    float v;
-                    if constexpr (PAGED) v = __builtin_amdgcn_cvt_f32_fp8(a.v_cache[au * D + d], 0);
-                    else v = bf16_to_f32(r.v[au * r.ld_v + (int64_t)kvh * D + d]);
-                    o[x] = fmaf(pu, v, o[x]);
-                }
+                if (d < D) o[x] = fmaf(pu, __builtin_amdgcn_cvt_f32_fp8(a.v_cache[au * D + d], 0), o[x]);
             }
         }
     }
-    uint16_t* out = (PAGED ? a.out + (int64_t)t * a.ld_out : r.out + (int64_t)t * r.ld_out) + (int64_t)head * D;
+    uint16_t* out = a.out + (int64_t)t * a.ld_out + (int64_t)head * D;
 #pragma unroll
     for (int x = 0; x < kMaxD / kWave; ++x) {
         const int d = lane + kWave * x;
@@ -165,44 +134,57 @@ __global__ __launch_bounds__(kRowThreads) void attention_row_kernel(PagedArgs a,
     }
 }
 
-}  // namespace
+__global__ __launch_bounds__(kRowThreads) void attention_row_kernel(PagedArgs a) {
+    __shared__ float qs[kRowWaves][kMaxD];
+    const int w = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int64_t items = (int64_t)a.T * a.Hq;
+    for (int64_t at = (int64_t)blockIdx.x * kRowWaves; at < items; at += (int64_t)gridDim.x * kRowWaves) {
+        const int64_t item = at + w;
+        const int t = (int)(item / a.Hq), head = (int)(item % a.Hq);
+        const int b = item < items ? seq_of(a.cu_q, a.T, a.B, t) : -1;
+        __syncthreads();                      // the last item's reads
+        if (b >= 0)
+            for (int d = lane; d < a.D; d += kWave) qs[w][d] = bf16_to_f32(a.q[(int64_t)t * a.ld_q + (int64_t)head * a.D + d]);
+        __syncthreads();
+        if (b >= 0) attend_row(a, qs[w], b, t, head);
+    }
+}
 
-namespace {
+// The lengths are the device's: never more workgroups than there are cells where every sequence fills its table.
+int workgroups(const PagedPlan& p, int64_t units, int64_t cells) {
+    return (int)std::min<int64_t>(std::min<int64_t>(units, p.groups) * cells, p.groups);
+}
 
 template <int DP, int NQ, int HG>
 hipError_t launch_stream(const PagedPlan& p, const PagedArgs& a, void* workspace, hipStream_t stream) {
     using C = StreamShape<DP, NQ, HG, 2, 4>;
-    // The lengths are the device's: never more workgroups than there are cells where every sequence fills its table.
     const int64_t units = ((int64_t)a.T * (a.Hq / a.H) / C::kRows + a.B) * ((a.H + HG - 1) / HG);
-    const int64_t cells = units * std::max<int64_t>(((a.max_len + C::kStep - 1) / C::kStep + 1) / kStreamCell, 1);
-    const int grid = (int)std::max<int64_t>(std::min<int64_t>(cells, p.groups), 1);
+    const int grid = workgroups(p, units, std::max<int64_t>(((a.max_len + C::kStep - 1) / C::kStep + 1) / kStreamCell, 1));
     float* const part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace) + kAttnTicketBytes);
     hipLaunchKernelGGL((paged_stream_kernel<DP, NQ, HG, 2, 4>), dim3(grid), dim3(256), C::kLds, stream, a, part,
                        reinterpret_cast<unsigned int*>(workspace), grid, C::KW == 1 ? 5 : 3);
     return hipGetLastError();
 }
 
-template <int DP, int W>
+template <int DP>
 hipError_t launch_tiles(const PagedPlan& p, const PagedArgs& a, void* workspace, hipStream_t stream) {
-    constexpr int kRows = 32 * W, kKeys = TileShape_<DP>::kKeys;
+    constexpr int kRows = 32 * kTileWaves<DP>, kKeys = TileShape_<DP>::kKeys;
     constexpr int kLds = std::max(PagedTileShape<DP>::kLds, kRows * DP * 4);
     const int64_t units = ((int64_t)a.T * (a.Hq / a.H) / kRows + a.B) * a.H;
-    const int64_t cells = units * std::max<int64_t>(((a.max_len + kKeys - 1) / kKeys + 1) / kTileCell, 1);
-    const int grid = (int)std::max<int64_t>(std::min<int64_t>(cells, p.groups), 1);
+    const int grid = workgroups(p, units, std::max<int64_t>(((a.max_len + kKeys - 1) / kKeys + 1) / kTileCell, 1));
     float* const part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace) + kAttnTicketBytes);
     unsigned int* const tickets = reinterpret_cast<unsigned int*>(workspace);
+    const dim3 block(64 * kTileWaves<DP>);
     if (a.per_tensor)
-        hipLaunchKernelGGL((paged_tile_kernel<DP, true, W>), dim3(grid), dim3(64 * W), kLds, stream, a, part, tickets, grid, 3);
+        hipLaunchKernelGGL((paged_tile_kernel<DP, true>), dim3(grid), block, kLds, stream, a, part, tickets, grid, 3);
     else
-        hipLaunchKernelGGL((paged_tile_kernel<DP, false, W>), dim3(grid), dim3(64 * W), kLds, stream, a, part, tickets, grid, 3);
+        hipLaunchKernelGGL((paged_tile_kernel<DP, false>), dim3(grid), block, kLds, stream, a, part, tickets, grid, 3);
     return hipGetLastError();
 }
 
 template <int DP>
-hipError_t launch_stream_rows(const PagedPlan& p, const PagedArgs& a, void* workspace, hipStream_t stream) {
-    if constexpr (DP == 128)
-        if (p.tile_waves == 8) return launch_tiles<DP, 8>(p, a, workspace, stream);
-    if (p.tile_waves == 4) return launch_tiles<DP, 4>(p, a, workspace, stream);
+hipError_t launch_paged(const PagedPlan& p, const PagedArgs& a, void* workspace, hipStream_t stream) {
+    if (p.tiles) return launch_tiles<DP>(p, a, workspace, stream);
     if (p.hg == 1)
         return p.nq == 1 ? launch_stream<DP, 1, 1>(p, a, workspace, stream) : launch_stream<DP, 2, 1>(p, a, workspace, stream);
     if (p.hg == 2)
@@ -217,32 +199,26 @@ hipError_t launch_paged_attention(const PagedArgs& given, void* workspace, hipSt
     if (a.num_blocks == 0) {             // no cache: every page is outside it, and loads need some address (q's first row)
         a.k_cache = a.v_cache = reinterpret_cast<const uint8_t*>(a.q);
         a.k_scale = a.v_scale = reinterpret_cast<const float*>(a.q);
+        a.per_tensor = 0;                // (a scale of a whole tensor would reach the sums)
     }
     const PagedPlan p = plan_paged(a.T, a.B, a.Hq, a.H, a.D, a.max_len);
-    if (p.dp == 64) return launch_stream_rows<64>(p, a, workspace, stream);
-    if (p.dp == 128) return launch_stream_rows<128>(p, a, workspace, stream);
-    if (p.dp == 256) return launch_stream_rows<256>(p, a, workspace, stream);
-    const int64_t items = (int64_t)a.T * a.Hq;
-    hipLaunchKernelGGL(attention_row_kernel<true>, dim3((unsigned)((items + kRowWaves - 1) / kRowWaves)),
-                       dim3(kRowThreads), 0, stream, a, PromptArgs{});
+    if (p.dp == 64) return launch_paged<64>(p, a, workspace, stream);
+    if (p.dp == 128) return launch_paged<128>(p, a, workspace, stream);
+    if (p.dp == 256) return launch_paged<256>(p, a, workspace, stream);
+    const int64_t blocks = std::min<int64_t>(((int64_t)a.T * a.Hq + kRowWaves - 1) / kRowWaves, (1 << 24) - 1);
+    hipLaunchKernelGGL(attention_row_kernel, dim3((unsigned)blocks), dim3(kRowThreads), 0, stream, a);
     return hipGetLastError();
 }
 
 hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t stream) {
-    const int64_t G = a.Hq / a.H, slots = (int64_t)a.T * G / 128 + a.B;
-    if (slots * a.H * 256 <= 0xffffffffll) {
-        const dim3 grid((unsigned)(slots * a.H)), block(256);
-        if (a.D > 128)
-            hipLaunchKernelGGL(prompt_tile_kernel<256>, grid, block, TileShape_<256>::kLds, stream, a, (int)slots);
-        else if (a.D <= 64)
-            hipLaunchKernelGGL(prompt_tile_kernel<64>, grid, block, TileShape_<64>::kLds, stream, a, (int)slots);
-        else
-            hipLaunchKernelGGL(prompt_tile_kernel<128>, grid, block, TileShape_<128>::kLds, stream, a, (int)slots);
-        return hipGetLastError();
-    }
-    const int64_t items = (int64_t)a.T * a.Hq;
-    hipLaunchKernelGGL(attention_row_kernel<false>, dim3((unsigned)((items + kRowWaves - 1) / kRowWaves)),
-                       dim3(kRowThreads), 0, stream, PagedArgs{}, a);
+    const int64_t slots = prompt_slots(a.T, a.B, a.Hq, a.H);
+    const dim3 grid((unsigned)(slots * a.H)), block(256);
+    if (a.D > 128)
+        hipLaunchKernelGGL(prompt_tile_kernel<256>, grid, block, TileShape_<256>::kLds, stream, a, (int)slots);
+    else if (a.D <= 64)
+        hipLaunchKernelGGL(prompt_tile_kernel<64>, grid, block, TileShape_<64>::kLds, stream, a, (int)slots);
+    else
+        hipLaunchKernelGGL(prompt_tile_kernel<128>, grid, block, TileShape_<128>::kLds, stream, a, (int)slots);
     return hipGetLastError();
 }
 

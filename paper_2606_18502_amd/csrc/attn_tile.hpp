@@ -460,6 +460,8 @@ struct RowBox {
     }
 };
 
+template <int DP>
+constexpr int kTileWaves = DP == 128 ? 8 : 4;                // of a paged tile's workgroup, 32 rows each
 constexpr int kTileCell = 8;                                 // steps that are worth a join of a whole tile's rows
 
 template <int DP>
@@ -468,11 +470,11 @@ struct PagedTileShape {
     static constexpr int kLds = kScales + 2 * (512 + 16);
 };
 
-template <int DP, bool PT, int W>
-__global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_tile_kernel(PagedArgs a, float* part, unsigned int* tickets,
+template <int DP, bool PT>
+__global__ __launch_bounds__(64 * kTileWaves<DP>, DP == 256 ? 1 : 2) void paged_tile_kernel(PagedArgs a, float* part, unsigned int* tickets,
                                                                             int groups, int extra) {
     using C = TileShape_<DP>;
-    constexpr int kThreads = 64 * W, kRows = 32 * W;
+    constexpr int kThreads = 64 * kTileWaves<DP>, kRows = 32 * kTileWaves<DP>;
     extern __shared__ __attribute__((aligned(1024))) uint8_t tile_smem[];
     __shared__ LineShared<kThreads> sh;
     const int tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6), h = lane >> 5, l32 = lane & 31;

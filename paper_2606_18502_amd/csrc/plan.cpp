@@ -2,11 +2,11 @@
 // GEMM, and the workspace layout of the acceptance.  Plain C++ (no HIP), so
 // the argument checks and plans can also be built and exercised on a host
 // without a GPU.
+#include <algorithm>
 #include <utility>
 
 #include "kernels.hpp"
 #include "plan.hpp"
-#include <stdlib.h>
 
 namespace specfp8 {
 
@@ -187,27 +187,34 @@ AcceptPlan plan_accept(int64_t B, int64_t k, int64_t V) {
     return p;
 }
 
+// Rows are those of an average sequence and one KV head.  Few rows stream the cache once past them, 16 or 32
+// at a time; many take tiles of 128 or 256 that share each key block, if there are enough tiles for half the
+// chip without cutting them (a part of a tile is 128 or 256 rows to join).  Tile / stream, us, 8 KV heads of
+// 4 query heads, contexts of 512..4096: 16 sequences at D = 128 of 256 rows 119/112, 384 170/153, 640 227/239,
+// 1024 295/384; at D = 64 of 96 rows 42.6/43.3, 128 47/50, 256 67/85; at D = 256 of 384 rows 414/396, 640
+// 628/629, 1024 968/988.  One sequence of 8000 tokens: 1024 rows (32 tiles) 106/90, 2048 148/135, 4096 (128)
+// 238/268; two of 4000: 1024 rows (64 tiles) 105/92, 2048 156/164.
 PagedPlan plan_paged(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t max_len) {
-    PagedPlan p{0, 0, 1, 0, 0, kAttnTicketBytes};
+    PagedPlan p{0, 0, 1, false, 0, kAttnTicketBytes};
     if (D % 16 != 0) return p;
     p.dp = D <= 64 ? 64 : (D <= 128 ? 128 : 256);
-    const int64_t rows = (T + B - 1) / B * (Hq / H);       // of an average sequence and one KV head
-    static const int64_t lim = getenv("AR") ? atoi(getenv("AR")) : 128, lim8 = getenv("A8") ? atoi(getenv("A8")) : 128;
-    if (rows > lim) {
-        p.tile_waves = p.dp == 128 && rows > lim8 ? 8 : 4;
-        p.groups = p.dp == 256 || p.tile_waves == 8 ? 256 : 512;
-        p.bytes += (size_t)p.groups * 2 * 32 * p.tile_waves * (p.dp + 4) * sizeof(float);
+    const int64_t rows = (T + B - 1) / B * (Hq / H), tile = p.dp == 128 ? 256 : 128;
+    if (rows > (p.dp == 64 ? 128 : 512) && B * ((rows + tile - 1) / tile) >= (128 + H - 1) / H) {
+        p.tiles = true;
+        p.groups = p.dp == 64 ? 512 : 256;
+        p.bytes += (size_t)p.groups * 2 * tile * (p.dp + 4) * sizeof(float);
         return p;
     }
+    // Rows of several 32s read the same keys: their workgroups share an L2, and smaller ones, two on a CU, hide
+    // more.  Heads together in a workgroup read longer runs of a slot (20 rows, 64 sequences: 88 us with two
+    // heads, 95 with one).
     p.nq = rows <= 16 ? 1 : 2;
     p.groups = rows > 32 ? 512 : 256;
     p.hg = H == 1 || rows > 32 ? 1 : (H == 2 || p.nq == 2 ? 2 : 4);
-    static const int ag = getenv("AG") ? atoi(getenv("AG")) : 0, ah = getenv("AH") ? atoi(getenv("AH")) : 0;
-    if (ag) p.groups = ag;
-    if (ah) p.hg = ah;
-    // a short line: one head a workgroup
-    if (B * ((H + p.hg - 1) / p.hg) * ((max_len * p.hg + 127) / 128) / 3 < p.groups) p.hg = 1;
-    p.bytes += (size_t)512 * 2 * 4 * 32 * (p.dp + 4) * sizeof(float);
+    p.bytes += (size_t)p.groups * 2 * p.hg * 16 * p.nq * (p.dp + 4) * sizeof(float);
+    // a short line has too few cells for the chip: one head a workgroup
+    const int64_t lines = std::min<int64_t>(B * ((H + p.hg - 1) / p.hg), 4 * p.groups);
+    if (lines * ((max_len * p.hg + 127) / 128) / 3 < p.groups) p.hg = 1;
     return p;
 }
 

@@ -99,11 +99,17 @@ constexpr int64_t kAcceptChunk = (int64_t)kAcceptThreads * kAcceptPerThread;   /
 constexpr size_t kAttnTicketBytes = 16384;   // at the start of the workspace, zero between calls
 
 // A call's kernel: D padded to dp (64, 128, 256; 0: the row kernel, for heads that are no multiple
-// of 16), 16*nq rows per unit, hg KV heads per workgroup.
+// of 16), either tiles of the matrix product (32 rows a wave) or a
+// stream of 16*nq rows of hg KV heads per workgroup.
 struct PagedPlan {
-    int dp, nq, hg, tile_waves, groups;
+    int dp, nq, hg;
+    bool tiles;
+    int groups;
     size_t bytes;          // of workspace: the tickets, then two parts per workgroup
 };
+// Workgroups along the rows of prompts (for each KV head).
+inline int64_t prompt_slots(int64_t T, int64_t B, int64_t Hq, int64_t H) { return T * (Hq / H) / 128 + B; }
+
 PagedPlan plan_paged(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t max_len);
 
 }  // namespace specfp8

@@ -3,6 +3,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include "plan.hpp"
+
 namespace specfp8 {
 
 namespace {
@@ -72,6 +74,7 @@ spec_status check_kv_cache_read(const void* k_cache, const void* v_cache, const 
                                 int mode, const int64_t* slot_mapping, int64_t T, int64_t H, int64_t D,
                                 int64_t num_slots, const void* k, int64_t ld_k, const void* v, int64_t ld_v) {
     // the write's rules; an empty cache has no rows to point at
+    if (H > 0 && D > 0 && D <= 512 && H > 0xffffffffLL / D) return SPEC_ERR_UNSUPPORTED;
     const bool empty = num_slots == 0;
     static const float unused = 0.0f;
     return check_kv_cache_write(k, ld_k, v, ld_v, slot_mapping, T, H, D, num_slots, mode,
@@ -133,6 +136,7 @@ spec_status check_prompt_attention(const void* q, int64_t ld_q, const void* k, i
     if (st != SPEC_OK) return st;
     if (ld_q < Hq * D || ld_out < Hq * D || ld_k < H * D || ld_v < H * D) return SPEC_ERR_SHAPE;
     if (T == 0 || B == 0) return SPEC_OK;
+    if (prompt_slots(T, B, Hq, H) > 0xffffff / H) return SPEC_ERR_UNSUPPORTED;      // a grid of fewer than 2^32 threads
     if (!q || !k || !v || !out || !cu_seqlens) return SPEC_ERR_NULL;
     if (ld_q % 8 != 0 || ld_k % 8 != 0 || ld_v % 8 != 0 || ld_out % 8 != 0) return SPEC_ERR_ALIGN;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned4(cu_seqlens))

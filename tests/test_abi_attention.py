@@ -45,6 +45,7 @@ def test_kv_cache_read(lib):
     assert read(lib, D=100, ld_k=800, ld_v=800) == UNSUP
     assert read(lib, D=520, ld_k=4160, ld_v=4160) == UNSUP
     assert read(lib, T=I31) == UNSUP
+    assert read(lib, H=1 << 25, ld_k=1 << 32, ld_v=1 << 32) == UNSUP        # H*D
     for name in ("kc", "vc", "ks", "vs", "slots", "k", "v"):
         assert read(lib, **{name: None}) == NULL, name
     for name in ("kc", "vc", "k", "v"):
@@ -117,7 +118,7 @@ def test_prompt_attention(lib):
     for bad in (dict(T=-1), dict(B=-1), dict(Hq=0), dict(H=0), dict(D=0), dict(H=5), dict(ld_q=4088), dict(ld_k=1016),
                 dict(ld_v=1016), dict(ld_out=4088)):
         assert prompt(lib, **bad) == SHAPE, bad
-    for bad in (dict(D=100), dict(D=264), dict(T=1 << 26), dict(B=I31)):
+    for bad in (dict(D=100), dict(D=264), dict(T=1 << 26), dict(B=I31), dict(B=1 << 21)):
         assert prompt(lib, **bad) == UNSUP, bad
     assert prompt(lib, scale=-0.5) == VALUE
     for name in ("q", "k", "v", "cu", "out"):

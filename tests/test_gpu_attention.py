@@ -44,7 +44,8 @@ def check_paged(c, what):
 # ------------------------------------------------------------------ the read
 
 @pytest.mark.parametrize("T,H,D,per_tensor", [(1, 1, 8, False), (5, 8, 128, False), (37, 3, 80, True), (13, 2, 24, False),
-                                              (9, 1, 512, True), (300, 4, 64, False)])
+                                              (9, 1, 512, True), (300, 4, 64, False), (11, 5, 512, False), (2100, 1, 40, False),
+                                              (7, 300, 8, False)])
 def test_kv_cache_read_is_exact(T, H, D, per_tensor):
     p = need_gpu()
     rng = np.random.default_rng(T)
@@ -114,6 +115,27 @@ def test_paged_chain(new, ctx, H, G, D, block, per_tensor):
                 f"paged new={new} ctx={ctx} H={H} G={G} D={D} block={block} per_tensor={per_tensor}")
 
 
+@pytest.mark.parametrize("new,ctx,H,G,D,block,per_tensor", [
+    ([65, 65], [0, 1], 32, 8, 128, 16, False),       # many rows: tiles of 256, nothing before them
+    ([300, 1, 37, 0, 90], [100, 600, 63, 40, 1], 16, 8, 128, 24, False),
+    ([70, 66], [640, 5], 32, 8, 128, 16, True),
+    ([80, 90], [129, 64], 32, 8, 112, 16, False),    # a head that ends inside its 128 columns
+    ([40] * 2, [63, 200], 32, 4, 64, 16, False),     # tiles of 128
+    ([129, 1, 70], [1000, 3, 64], 16, 5, 48, 8, True),
+    ([65, 70, 65], [30, 300, 2], 16, 8, 256, 16, False),
+    ([65, 70, 65], [30, 300, 2], 16, 8, 192, 100, True),
+])
+def test_paged_tiles_of_many_rows(new, ctx, H, G, D, block, per_tensor):
+    check_paged(paged_case(len(new) + D, new, ctx, H, G, D, block, per_tensor),
+                f"paged tiles new={new} ctx={ctx} H={H} G={G} D={D} block={block} per_tensor={per_tensor}")
+
+
+@pytest.mark.parametrize("per_tensor", [False, True])
+def test_paged_tiles_of_which_a_few_are_long(per_tensor):
+    """One row group of 30000 tokens among short ones: its tile is cut into more parts than one workgroup joins."""
+    check_paged(paged_case(25, [1, 130, 130], [30000, 20, 7], 4, 32, 128, per_tensor=per_tensor), "one long tile")
+
+
 def test_paged_no_tokens_fewer_tokens_than_rows_and_lengths_outside():
     p = need_gpu()
     c = paged_case(3, [3, 3, 3, 3, 3], [10, 4, 6, 13, 0], 2, 2, 64)
@@ -138,9 +160,31 @@ def test_paged_tables_that_point_outside():
     assert (out == 0).all()
 
 
+@pytest.mark.parametrize("per_tensor", [False, True])
+@pytest.mark.parametrize("new,H,G,D", [([4, 4], 2, 4, 128), ([65, 65], 32, 8, 128), ([40, 40], 32, 4, 64), ([3, 3], 2, 2, 24)])
+def test_paged_pages_outside_and_no_cache(new, H, G, D, per_tensor):
+    """The same for few rows, for tiles and for the smallest heads; then a cache without a page, whose scales are NaN."""
+    p = need_gpu()
+    c = paged_case(29, new, [120, 40], H, G, D, per_tensor=per_tensor)
+    c["tables"][0, 1] = 10 ** 9
+    c["tables"][0, 4] = -1
+    c["tables"][1, :] = -5
+    ref, tol = paged_reference(c)
+    d = on_device(c)
+    out = values(call(p, c, d))
+    assert (out[new[0]:] == 0).all() and within(out, ref, tol) <= 1.0
+    c["ks"][:] = np.nan
+    c["vs"][:] = np.nan
+    c["kc"], c["vc"] = c["kc"][:0], c["vc"][:0]
+    if not per_tensor:
+        c["ks"], c["vs"] = c["ks"][:0], c["vs"][:0]
+    assert (values(call(p, c, on_device(c))) == 0).all()
+
+
 @pytest.mark.parametrize("N,ctx,H,G,D,per_tensor", [(1, [0, 40], 1, 1, 64, False), (4, [1, 33], 2, 4, 128, False),
                                                     (25, [700, 64], 2, 4, 128, False), (63, [5], 1, 4, 128, True),
-                                                    (64, [0, 100], 1, 2, 96, False), (33, [31], 3, 1, 256, False)])
+                                                    (64, [0, 100], 1, 2, 96, False), (33, [31], 3, 1, 256, False),
+                                                    (64, [3, 90], 32, 8, 128, False), (64, [3, 90], 32, 4, 64, True)])
 def test_paged_tree(N, ctx, H, G, D, per_tensor):
     p = need_gpu()
     rng = np.random.default_rng(N)
@@ -164,19 +208,18 @@ def test_a_chain_shaped_tree_is_the_chain():
     assert torch.equal(call(p, c, d), chain)
 
 
-@pytest.mark.parametrize("where", ["K code", "V code", "K scale", "V scale"])
-@pytest.mark.parametrize("new", [[4], [40]])
-@pytest.mark.parametrize("tree", [False, True])
-def test_a_nan_reaches_the_rows_that_see_it_and_no_others(where, new, tree):
+def a_nan_reaches(where, new, tree, H, G, D):
+    """Of the first sequence's second KV head."""
     p = need_gpu()
     n = new[0]
-    parents = np.array([[-1, -1] + [m % 2 for m in range(n - 3)]], np.int32)
-    masks = ot.tree_attention_masks(parents)[0] if tree else None
-    c = paged_case(11, new, [70], 2, 4, 128, tree=masks)
+    masks = None
+    if tree:
+        parents = np.array([[-1, -1] + [m % 2 for m in range(n - 3)]] * len(new), np.int32)
+        masks = ot.tree_attention_masks(parents)[0]
+    c = paged_case(11, new, [70] * len(new), H, G, D, tree=masks)
     L = int(c["lens"][0])
     j = L - n + 2                                        # the second node, or the third token of the chain
     slot = c["tables"][0, j // 16] * 16 + j % 16
-    clean, _ = paged_reference(c)
     before = values(call(p, c, on_device(c)))
     if where == "K code":
         c["kc"][slot, 1, 5] = CODE_NAN
@@ -187,17 +230,32 @@ def test_a_nan_reaches_the_rows_that_see_it_and_no_others(where, new, tree):
     else:
         c["vs"][slot, 1] = np.inf
     out = values(call(p, c, on_device(c)))
-    seen = (oa.tree_seen([int(m) for m in masks[0]], L) if tree else oa.chain_seen(n, L))[:, j]
-    assert seen.any() and not seen.all()
+    seen = np.zeros(out.shape[0], bool)
+    seen[:n] = (oa.tree_seen([int(m) for m in masks[0]], L) if tree else oa.chain_seen(n, L))[:, j]
+    assert seen.any() and not seen[:n].all()
     hit = np.zeros(out.shape, bool)
-    hit[seen, 4:] = True                                 # the second KV head's query heads
+    hit[seen, G:2 * G] = True                            # the second KV head's query heads
     np.testing.assert_array_equal(out[~hit], before[~hit])
     if where == "V code":                                # its channel alone
-        assert np.isnan(out[seen][:, 4:, 5]).all()
-        others = np.delete(np.arange(128), 5)
+        assert np.isnan(out[seen][:, G:2 * G, 5]).all()
+        others = np.delete(np.arange(D), 5)
         assert np.isfinite(out[:, :, others]).all()
     else:
-        assert not np.isfinite(out[seen][:, 4:]).any()
+        assert not np.isfinite(out[seen][:, G:2 * G]).any()
+
+
+@pytest.mark.parametrize("where", ["K code", "V code", "K scale", "V scale"])
+@pytest.mark.parametrize("new", [[4], [40]])
+@pytest.mark.parametrize("tree", [False, True])
+def test_a_nan_reaches_the_rows_that_see_it_and_no_others(where, new, tree):
+    a_nan_reaches(where, new, tree, 2, 4, 128)
+
+
+@pytest.mark.parametrize("where", ["K code", "V code", "K scale", "V scale"])
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("new,H,G,D", [([65, 65], 32, 8, 128), ([40, 40], 32, 4, 64), ([65, 65], 16, 8, 256)])
+def test_a_nan_and_tiles_of_rows(where, tree, new, H, G, D):
+    a_nan_reaches(where, new, tree, H, G, D)
 
 
 def test_paged_strides_and_rows_of_no_sequence():
@@ -279,7 +337,8 @@ def test_one_workspace_for_calls_of_different_shapes_and_the_same_results_twice(
     p = need_gpu()
     cases = [paged_case(20, [1], [5000], 1, 4, 128), paged_case(21, [5] * 6, [900, 30, 0, 2000, 77, 400], 2, 4, 128),
              paged_case(22, [100, 1], [300, 1500], 2, 2, 64), paged_case(23, [1] * 3, [10, 20, 30], 4, 1, 256),
-             paged_case(24, [26] * 2, [600, 1200], 1, 4, 128)]
+             paged_case(24, [26] * 2, [600, 1200], 1, 4, 128), paged_case(26, [65] * 2, [600, 1200], 32, 8, 128),
+             paged_case(27, [40] * 4, [900, 1100, 0, 5], 8, 4, 64), paged_case(28, [3] * 2, [90, 20], 2, 2, 24)]
     need = [p.paged_attention_workspace_bytes(c["T"], len(c["lens"]), c["H"] * c["G"], c["H"], c["D"]) for c in cases]
     ws = torch.zeros(max(need), dtype=torch.uint8, device="cuda")
     ws[16384:] = 0xFF                                    # only the tickets have to be zero
