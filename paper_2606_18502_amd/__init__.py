@@ -10,8 +10,11 @@ Beside the chain verify step it offers the LM-head GEMM with the acceptance
 statistics in its epilogue (gemm_logit_stats, then verify_accept with
 target_stats), the gate|up GEMM with the SiLU gate in its epilogue
 (gemm_silu_mul), token-tree verification (verify_accept_tree) with its
-attention masks (tree_attention_mask), and the
-FP8 KV-cache write of the new tokens' keys and values (kv_cache_write).
+attention masks (tree_attention_mask), the FP8 KV-cache write of the new
+tokens' keys and values (kv_cache_write) and its reverse (kv_cache_read), the
+attention of new tokens, drafted chains and trees over that paged cache
+(paged_attention), and the causal attention of the packed prompts that fill it
+(prompt_attention).
 
 The computation lives in libspecfp8.so (HIP kernels behind the C ABI of
 include/spec_fp8.h); this package only marshals torch tensors into that ABI.

@@ -1,13 +1,6 @@
-// Tree attention masks for token-tree verification: for every node of a
-// drafted tree, the set of tree nodes its row may attend to (the nodes on the
-// path from the root to it, itself included) as a 64-bit mask, and its depth.
-//
-// One wave per sequence, lane n owning node n (N <= 64).  The masks come from
-// pointer jumping over the parent links: after step s every lane holds the
-// nodes within 2^s - 1 steps above it and a pointer to its 2^s-th ancestor,
-// so six steps of lane exchanges (no memory traffic) cover any depth up to
-// 64.  A node whose parent is not one of the earlier nodes (or -1) poisons
-// itself and, through the same exchanges, every node below it.
+// Tree attention masks, and the launches of the attentions: over the paged FP8 cache
+// (attn_stream.hpp for few rows, attn_tile.hpp for many, the kernel below for heads
+// whose codes are no whole 16-byte pieces) and over packed prompts (attn_tile.hpp).
 #include <algorithm>
 
 #include "attn_common.hpp"
@@ -18,6 +11,16 @@ namespace specfp8 {
 
 namespace {
 
+// ---- tree masks: for token-tree verification, for every node of a
+// drafted tree, the set of tree nodes its row may attend to (the nodes on the
+// path from the root to it, itself included) as a 64-bit mask, and its depth.
+//
+// One wave per sequence, lane n owning node n (N <= 64).  The masks come from
+// pointer jumping over the parent links: after step s every lane holds the
+// nodes within 2^s - 1 steps above it and a pointer to its 2^s-th ancestor,
+// so six steps of lane exchanges (no memory traffic) cover any depth up to
+// 64.  A node whose parent is not one of the earlier nodes (or -1) poisons
+// itself and, through the same exchanges, every node below it.
 constexpr int kTmThreads = 256;
 constexpr int kTmSeqPerBlock = kTmThreads / 64;
 
@@ -76,7 +79,6 @@ __device__ __forceinline__ int seq_of(const int32_t* cu, int T, int B, int t) {
 // Heads whose rows are not whole 16-byte pieces of codes (D % 16 == 8): one wave per (row, query head),
 // lanes over 64 keys for the scores, then over D for the sums.  All fp32 on the vector units, 64 keys a step,
 // the running maximum and sum of the softmax; bounded by its dot products (every wave reads its keys again).
-// ROW_FIGURES
 __device__ __forceinline__ void attend_row(const PagedArgs& a, const float* qs, int b, int t, int head) {
     const int lane = threadIdx.x % kWave, D = a.D, H = a.H, kvh = head / (a.Hq / H);
     int first, n;
