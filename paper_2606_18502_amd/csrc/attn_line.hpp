@@ -45,10 +45,15 @@ struct Line {
     static __device__ __forceinline__ int64_t units(const PagedArgs& a, int n, int nhg) {
         return (((int64_t)n * (a.Hq / a.H) + ROWS - 1) / ROWS) * nhg;
     }
-    static __device__ __forceinline__ int64_t cost_of(const PagedArgs& a, int b, int nhg, int extra) {
-        int first, n;
-        rows_of(a.cu_q, a.T, a.B, b, &first, &n);
-        return units(a, n, nhg) * length(max((min(max(a.kv_lens[b], 0), a.max_len) + STEP - 1) / STEP, 1), extra);
+    struct Sequence {
+        int first, n, L;
+        __device__ __forceinline__ Sequence(const PagedArgs& a, int b) {
+            rows_of(a.cu_q, a.T, a.B, b, &first, &n);
+            L = min(max(a.kv_lens[b], 0), a.max_len);
+        }
+    };
+    static __device__ __forceinline__ int64_t cost_of(const PagedArgs& a, const Sequence& s, int nhg, int extra) {
+        return units(a, s.n, nhg) * length(max((s.L + STEP - 1) / STEP, 1), extra);
     }
     static __device__ __forceinline__ int64_t sum_before(int64_t mine, int64_t* scan, int64_t* sum) {
         const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -73,9 +78,10 @@ struct Line {
         const int tid = threadIdx.x;
         nhg = (a.H + heads - 1) / heads;
         const int per = (a.B + THREADS - 1) / THREADS;
+        const Sequence own(a, min(tid * per, a.B - 1));      // (the first of this thread's; mostly the only one)
         const auto sum_here = [&](int how) {
-            int64_t v = 0;
-            for (int x = 0; x < per && tid * per + x < a.B; ++x) v += cost_of(a, tid * per + x, nhg, how);
+            int64_t v = tid * per < a.B ? cost_of(a, own, nhg, how) : 0;
+            for (int x = 1; x < per && tid * per + x < a.B; ++x) v += cost_of(a, Sequence(a, tid * per + x), nhg, how);
             return v;
         };
         extra = -1;
@@ -101,7 +107,7 @@ struct Line {
         if (pos >= before && pos < before + mine) {
             int64_t at = before;
             for (int x = 0; x < per; ++x) {
-                const int64_t c = cost_of(a, tid * per + x, nhg, extra);
+                const int64_t c = cost_of(a, x == 0 ? own : Sequence(a, tid * per + x), nhg, extra);
                 if (pos < at + c) {
                     sh.found[0] = tid * per + x;
                     sh.found[1] = at;
@@ -114,7 +120,18 @@ struct Line {
         b = uniform((int)sh.found[0]);
         base = uniform(sh.found[1]);
         window_at = b - 32;
+        if (per == 1) {
+            window_at = b;
+            if (tid >= b && tid < b + 32) to_window(own, sh, tid - b);       // (past the last sequence: not looked at)
+            __syncthreads();
+        }
         return true;
+    }
+
+    static __device__ __forceinline__ void to_window(const Sequence& s, LineShared<THREADS>& sh, int at) {
+        sh.window[0][at] = s.first;
+        sh.window[1][at] = s.n;
+        sh.window[2][at] = s.L;
     }
 
     // The next segment; false at the end of the range.  Called by all threads.
@@ -123,13 +140,8 @@ struct Line {
             if (b >= window_at + 32) {
                 window_at = b;
                 __syncthreads();
-                if (threadIdx.x < 32 && b + (int)threadIdx.x < a.B) {
-                    int f, c;
-                    rows_of(a.cu_q, a.T, a.B, b + (int)threadIdx.x, &f, &c);
-                    sh.window[0][threadIdx.x] = f;
-                    sh.window[1][threadIdx.x] = c;
-                    sh.window[2][threadIdx.x] = min(max(a.kv_lens[b + (int)threadIdx.x], 0), a.max_len);
-                }
+                if (threadIdx.x < 32 && b + (int)threadIdx.x < a.B)
+                    to_window(Sequence(a, b + (int)threadIdx.x), sh, (int)threadIdx.x);
                 __syncthreads();
             }
             first = uniform(sh.window[0][b - window_at]);

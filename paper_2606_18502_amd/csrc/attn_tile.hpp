@@ -342,19 +342,21 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void prompt_tile_kernel(Pro
     // belongs to takes one comparison per prompt.  Late tiles, the longest, go first; heads go round-robin over the
     // XCDs, so that a KV head's tiles share an L2.
     const int head = blockIdx.x % a.H, slot = slots - 1 - (int)(blockIdx.x / a.H);
-    int b = -1;
+    int b = -1, first = 0, n = 0;
     for (int x = 0; x < a.B; x += 64) {
         const int y = x + lane;
-        const bool at = y < a.B && (int64_t)min(max(a.cu[min(y, a.B)], 0), a.T) * G / C::kRows + y <= slot;
-        const uint64_t votes = __ballot(at);
-        if (votes) b = x + 63 - __builtin_clzll(votes);
+        int lo, rows;
+        rows_of(a.cu, a.T, a.B, min(y, a.B - 1), &lo, &rows);
+        const uint64_t votes = __ballot(y < a.B && (int64_t)lo * G / C::kRows + y <= slot);
+        if (votes) {
+            const int last = 63 - __builtin_clzll(votes);
+            b = x + last;
+            first = __builtin_amdgcn_readlane(lo, last);
+            n = __builtin_amdgcn_readlane(rows, last);
+        }
         if (votes != ~0ull) break;
     }
     if (b < 0) return;
-    int first, n;
-    rows_of(a.cu, a.T, a.B, b, &first, &n);
-    first = uniform(first);
-    n = uniform(n);
     const int tile = slot - (int)((int64_t)first * G / C::kRows + b);
     const int64_t row0 = (int64_t)tile * C::kRows;
     if (tile < 0 || row0 >= (int64_t)n * G) return;
