@@ -460,10 +460,16 @@ SPEC_PY(py_paged_attention) {
     const size_t bytes = spec_fp8_paged_attention_workspace_bytes(h.T, B, h.H, c.H, h.D);
     Tensor ws;
     if (a[13] != Py_None) {
-        const Tensor& w = any_tensor(a[13], "workspace");
+        const Tensor& w = dev_any(a[13], "workspace");
+        same_device(w, q, "workspace");
+        need(w.is_contiguous(), "workspace must be contiguous");
         if ((size_t)bytes_of(w) >= bytes) ws = w;
     }
-    if (!ws.defined()) ws = at::zeros({(int64_t)std::max<size_t>(bytes, 1)}, q.options().dtype(ScalarType::Byte));
+    if (!ws.defined()) {
+        const int64_t size = std::max<int64_t>((int64_t)bytes, 1);
+        ws = at::empty({size}, q.options().dtype(ScalarType::Byte));
+        ws.narrow(0, 0, std::min<int64_t>(size, 16384)).zero_();             // the tickets
+    }
     void* const s = stream();
     check("spec_fp8_paged_attention", call([&] {
               return spec_fp8_paged_attention(

@@ -110,7 +110,7 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     [cu_q[0], cu_q[B]) stay as they were (a new one holds anything there).
     workspace: paged_attention_workspace_bytes(T, B, Hq, H, D) bytes on the GPU, 16-byte
     aligned, zero-filled once and then kept for all calls of a stream.  Bring
-    one: without it (or with one too small) every call zero-fills a new one.
+    one: without it (or with one too small) every call makes a new one.
     """
     return (_bind or _load_bind()).paged_attention(q, k_cache, v_cache, k_scale, v_scale, block_tables, kv_lens,
                                                    block_size, cu_q, tree_mask, scale, per_tensor, out, workspace)

@@ -509,6 +509,8 @@ def test_refused_arguments():
         (lambda: call(p, c, dict(d, tree=torch.zeros((2, 1), dtype=torch.int64, **z), cu=dev_i32([0, 2, 4]))), "cu_q must be None"),
         (lambda: call(p, c, d, out=torch.empty((4, 4, 32), dtype=torch.bfloat16, **z)), "out must be"),
         (lambda: call(p, c, d, scale="steep"), "could not convert"),
+        (lambda: call(p, c, d, workspace=torch.zeros(1 << 24, dtype=torch.uint8)), "workspace must be"),
+        (lambda: call(p, c, d, workspace=torch.zeros((1 << 12, 1 << 12), dtype=torch.uint8, **z).t()), "workspace must be contiguous"),
         (lambda: p.prompt_attention(d["q"], d["q"][:, :2], d["q"][:3, :2], dev_i32([0, 4])), "k and v must be"),
         (lambda: p.prompt_attention(d["q"], d["q"], d["q"], dev_i32([[0, 4]])), "cu_seqlens"),
         (lambda: p.kv_cache_read(d["kc"], d["vc"], dev_i32([0]), d["ks"], d["vs"]), "slot_mapping must have dtype"),
