@@ -508,7 +508,8 @@ spec_status spec_fp8_kv_cache_read(const uint8_t* k_cache, const uint8_t* v_cach
  * of -inf, is zeros.  What a row does not see has no influence on it, NaN codes and scales
  * included.  Products of q and codes are exact; they are summed, and the sums
  * of p and p*v accumulated, in fp32; p_ij * sv_j (or p_ij alone, where one
- * scale holds for the tensor) is rounded to bf16 (to nearest) for the second product.
+ * scale holds for the tensor) enters the second product as bf16: as the sum of two for few
+ * rows, rounded to nearest for many.
  *
  * q        bf16 [T, ld_q], head h at columns [h*D, (h+1)*D).  The rows of sequence b are
  *          cu_q[b] .. cu_q[b+1]-1, or with cu_q NULL T/B rows each (T % B == 0,

@@ -23,7 +23,7 @@
 //
 // What bounds it: the cache's bytes.  At 8 KV heads of 128, 4 query heads each: two contexts of 95000 tokens
 // and one row each take 87 us (402 MB, 4.7 TB/s with the start and the join; 5.8 to 6.2 inside the loop), 64
-// of 512..4096 tokens 68 us with one row each and 88 with five: there every range begins two units or more
+// of 512..4096 tokens 68 us with one row each and 90 with five: there every range begins two units or more
 // (queries, tables, the first codes: loads that depend on each other, ~9 us) and joins its parts.  Not faster:
 // rings of 3 and 4 stages, eight waves a workgroup, a raised wave priority.
 #pragma once
@@ -301,7 +301,9 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
                     }
                 }
                 // ---- probabilities, as the second product's operand
-                bf16x8_t pv[NQ];
+                // (in two halves, the upper 8 bits of each and bf16 of the rest: one half alone adds as much error to a
+                // row as the output's own rounding, and for few keys the same one to all its channels)
+                bf16x8_t pv[NQ], rest[NQ];
 #pragma unroll
                 for (int x = 0; x < NQ; ++x) {
                     float p0[4], p1[4];
@@ -320,12 +322,16 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
                             p1[r] = (seen[x] >> (16 + r)) & 1 ? p1[r] : 0.0f;
                         }
                     }
-                    u32x4_t v;
-                    v[0] = f32_to_bf16x2(p0[0], p0[1]);
-                    v[1] = f32_to_bf16x2(p0[2], p0[3]);
-                    v[2] = f32_to_bf16x2(p1[0], p1[1]);
-                    v[3] = f32_to_bf16x2(p1[2], p1[3]);
+                    u32x4_t v, y;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float lo = r < 2 ? p0[2 * r] : p1[2 * r - 4], hi = r < 2 ? p0[2 * r + 1] : p1[2 * r - 3];
+                        const uint32_t lo_up = __float_as_uint(lo) & 0xffff0000u, hi_up = __float_as_uint(hi) & 0xffff0000u;
+                        v[r] = hi_up | (lo_up >> 16);
+                        y[r] = f32_to_bf16x2(lo - __uint_as_float(lo_up), hi - __uint_as_float(hi_up));
+                    }
                     pv[x] = __builtin_bit_cast(bf16x8_t, v);
+                    rest[x] = __builtin_bit_cast(bf16x8_t, y);
                 }
                 // ---- sums of values
                 if (!full) {
@@ -373,8 +379,10 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
                 for (int d = 0; d < NB; ++d) {
                     const bf16x8_t vt = codes_to_bf16((uint32_t)vc[d][0], (uint32_t)vc[d][1]);
 #pragma unroll
-                    for (int x = 0; x < NQ; ++x)
+                    for (int x = 0; x < NQ; ++x) {
                         o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pv[x], o[x][d], 0, 0, 0);
+                        o[x][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, rest[x], o[x][d], 0, 0, 0);
+                    }
                 }
             };
 

@@ -190,16 +190,16 @@ AcceptPlan plan_accept(int64_t B, int64_t k, int64_t V) {
 // Rows are those of an average sequence and one KV head.  Few rows stream the cache once past them, 16 or 32
 // at a time; many take tiles of 128 or 256 that share each key block, if there are enough tiles for half the
 // chip without cutting them (a part of a tile is 128 or 256 rows to join).  Tile / stream, us, 8 KV heads of
-// 4 query heads, contexts of 512..4096: 16 sequences at D = 128 of 256 rows 119/112, 384 170/153, 640 227/239,
-// 1024 295/384; at D = 64 of 96 rows 42.6/43.3, 128 47/50, 256 67/85; at D = 256 of 384 rows 414/396, 640
-// 628/629, 1024 968/988.  One sequence of 8000 tokens: 1024 rows (32 tiles) 106/90, 2048 148/135, 4096 (128)
-// 238/268; two of 4000: 1024 rows (64 tiles) 105/92, 2048 156/164.
+// 4 query heads, contexts of 512..4096.  16 sequences at D = 128 of 128 rows 92/77, 192 106/102, 256 124/140,
+// 640 228/283, 1024 298/443, and 64 sequences of 192 rows 284/359; at D = 64 of 64 rows 37/34, 80 41/42, 128
+// 46/52, 256 66/88; at D = 256 of 192 rows 300/244, 256 306/302, 384 412/420, 1024 970/1061.  Few tiles: 8
+// sequences of 256 rows (64 tiles) 93/83, 4 of 512 (64) 98/94, 2 of 1024 (64) 104/104, one of 2048 (64) 140/159.
 PagedPlan plan_paged(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t max_len) {
     PagedPlan p{0, 0, 1, false, 0, kAttnTicketBytes};
     if (D % 16 != 0) return p;
     p.dp = D <= 64 ? 64 : (D <= 128 ? 128 : 256);
     const int64_t rows = (T + B - 1) / B * (Hq / H), tile = p.dp == 128 ? 256 : 128;
-    if (rows > (p.dp == 64 ? 128 : 512) && B * ((rows + tile - 1) / tile) >= (128 + H - 1) / H) {
+    if (rows >= (p.dp == 64 ? 80 : p.dp == 128 ? 192 : 257) && B * ((rows + tile - 1) / tile) >= (128 + H - 1) / H) {
         p.tiles = true;
         p.groups = p.dp == 64 ? 512 : 256;
         p.bytes += (size_t)p.groups * 2 * tile * (p.dp + 4) * sizeof(float);
