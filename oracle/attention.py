@@ -102,11 +102,12 @@ def prompt_attention(q, k, v, cu, scale):
     return out, spread, mag
 
 
-def bound(out, spread, mag, D, L):
+def bound(out, spread, mag, D, L, weight=2.0 ** -8):
     """How far a kernel's bf16 output may be from `out`, element by element.
 
     Half a bf16 step of the result (2^-8 |out|); every p_ij (times its value
-    scale) rounded to bf16 once, 2^-8 of its term at most: 2^-8 spread; a score
+    scale) rounded to bf16 once, `weight` = 2^-8 of its term at most: 2^-8 spread
+    (as the sum of two, 8 bits and the rest of at most 2^-7 rounded: 2^-15); a score
     is a sum of D exact products in fp32 with the scales and log2(e) as further
     factors and the reference subtracted: (D + 8) 2^-23 of mag (its absolute terms,
     an addition taken to cut its result; the reference is within 8 of the largest:
@@ -115,7 +116,7 @@ def bound(out, spread, mag, D, L):
     (L + 4) 2^-23 each, twice."""
     score = (D + 8) * 2.0 ** -23 * (mag + 8.0)[..., None]
     sums = (L + 4) * 2.0 ** -23
-    rel = np.expm1(2 * score) + 2 * sums + 2.0 ** -8
+    rel = np.expm1(2 * score) + 2 * sums + weight
     return 2.0 ** -8 * np.abs(out) * (1 + rel) + spread * rel + 2.0 ** -126
 
 

@@ -278,6 +278,19 @@ def test_paged_strides_and_rows_of_no_sequence():
     assert (back[:, :8] == 5).all() and (back[:, 8 + Hq * D:] == 5).all()
 
 
+@pytest.mark.parametrize("new,ctx,H,G,D", [([1, 1, 1], [0, 1, 700], 4, 4, 128), ([5, 5], [2, 300], 2, 4, 64),
+                                            ([26], [90], 2, 4, 128), ([2, 3], [40, 0], 1, 2, 256)])
+def test_weights_of_few_rows_are_kept_to_15_bits(new, ctx, H, G, D):
+    p = need_gpu()
+    c = paged_case(17, new, ctx, H, G, D)
+    say(f"weights new={new} ctx={ctx} H={H} G={G} D={D}")
+    rows = [(int(a), int(e - a)) for a, e in zip(c["cu"][:-1], c["cu"][1:])]
+    out, spread, mag = oa.paged_attention(c["q"], c["kc"], c["vc"], c["ks"], c["vs"], c["tables"], c["lens"], c["block"],
+                                          c["scale"], rows, None)
+    tol = oa.bound(out, spread, mag, D, int(c["lens"].max()), weight=2.0 ** -15)
+    assert within(values(call(p, c, on_device(c))), out, tol) <= 1.0
+
+
 @pytest.mark.parametrize("scale", [1e-3, 40.0])
 def test_paged_flat_and_steep_scores(scale):
     """Nearly equal weights, and scores of thousands, where one key takes nearly all."""
