@@ -506,7 +506,8 @@ spec_status spec_fp8_kv_cache_read(const uint8_t* k_cache, const uint8_t* v_cach
  *
  * over the tokens seen (m_i: a reference within 2^8 of the largest s_ij); a row that sees none, or only scores
  * of -inf, is zeros.  What a row does not see has no influence on it, NaN codes and scales
- * included.  Products of q and codes are exact; they are summed, and the sums
+ * included.  An infinite scale of a value seen gives infinities of its codes' signs, NaN where
+ * the code is 0.  Products of q and codes are exact; they are summed, and the sums
  * of p and p*v accumulated, in fp32; p_ij * sv_j (or p_ij alone, where one
  * scale holds for the tensor) enters the second product as bf16: as the sum of two for few
  * rows, rounded to nearest for many.

@@ -257,6 +257,11 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
                 const f32x4_t sk1 = *reinterpret_cast<const f32x4_t*>(sc + 16 + 4 * qd) * c2;
                 const f32x4_t sv0 = *reinterpret_cast<const f32x4_t*>(sc + 32 + 4 * qd);
                 const f32x4_t sv1 = *reinterpret_cast<const f32x4_t*>(sc + 48 + 4 * qd);
+                // (p < 2^8: a product with a value scale below this is finite, and so is what the upper half leaves)
+                float sv_top = fmaxf(fabsf(sv0[0]), fabsf(sv1[0]));
+#pragma unroll
+                for (int r = 1; r < 4; ++r) sv_top = fmaxf(sv_top, fmaxf(fabsf(sv0[r]), fabsf(sv1[r])));
+                const bool huge = __ballot(sv_top >= 0x1p119f) != 0;
                 uint32_t seen[NQ];
                 float top[NQ];
                 bool over = false;
@@ -329,6 +334,13 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
                         const uint32_t lo_up = __float_as_uint(lo) & 0xffff0000u, hi_up = __float_as_uint(hi) & 0xffff0000u;
                         v[r] = hi_up | (lo_up >> 16);
                         y[r] = f32_to_bf16x2(lo - __uint_as_float(lo_up), hi - __uint_as_float(hi_up));
+                    }
+                    if (huge) {                          // an infinite product is its upper half alone (inf - inf is NaN)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            if ((v[r] & 0x7f80u) == 0x7f80u) y[r] &= 0xffff0000u;
+                            if ((v[r] & 0x7f800000u) == 0x7f800000u) y[r] &= 0xffffu;
+                        }
                     }
                     pv[x] = __builtin_bit_cast(bf16x8_t, v);
                     rest[x] = __builtin_bit_cast(bf16x8_t, y);

@@ -271,15 +271,24 @@ __device__ __forceinline__ void clean_part(uint8_t* tile) {
     }
 }
 
-// Keys that are not there have values 0; keys whose value scale is infinite or NaN have NaN values and no weight.
+// Keys that are not there have values 0; keys whose value scale is infinite or NaN have their values scaled by it
+// here (infinite or NaN, so that they are marked) and no weight.
 template <int DP>
 __device__ __forceinline__ void settle_part(uint8_t* tile, uint64_t there, const float* v_scales) {
 #pragma unroll 1
     for (int x = threadIdx.x * 16; x < TileShape_<DP>::kTile; x += blockDim.x * 16) {
         const int key = x / (2 * DP);
         u32x4_t* const at = reinterpret_cast<u32x4_t*>(tile + x);
-        if (!((there >> key) & 1)) *at = u32x4_t{0, 0, 0, 0};
-        else if (v_scales && !(fabsf(v_scales[key]) < INFINITY)) *at = u32x4_t{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+        if (!((there >> key) & 1)) {
+            *at = u32x4_t{0, 0, 0, 0};
+        } else if (v_scales && !(fabsf(v_scales[key]) < INFINITY)) {
+            const float f = v_scales[key];
+            u32x4_t v = *at;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = f32_to_bf16x2(__uint_as_float(v[e] << 16) * f, __uint_as_float(v[e] & 0xffff0000u) * f);
+            *at = v;
+        }
     }
 }
 

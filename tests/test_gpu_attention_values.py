@@ -1,0 +1,66 @@
+"""Infinite, NaN and zero values and scales in the attentions: every path has to give what the formula gives in IEEE
+arithmetic, wherever the key lies, and zeros for a row that sees nothing."""
+
+import numpy as np
+import pytest
+import torch
+
+import workloads as wl
+from oracle import attention as oa, e4m3, tree as ot
+from tests.attention_cases import paged_case, paged_reference, within
+from tests.gpu_util import dev_bf16, dev_f32, dev_i32, dev_u8, host_bf16_bits, need_gpu, say
+
+pytestmark = pytest.mark.gpu
+
+
+def values(t):
+    return wl.f32_from_bf16_bits(host_bf16_bits(t)).astype(np.float64)
+
+
+def run(p, c):
+    tree = None if c["tree"] is None else torch.from_numpy(c["tree"].view(np.int64).copy()).cuda()
+    return values(p.paged_attention(dev_bf16(c["q_bits"]), dev_u8(c["kc"]), dev_u8(c["vc"]), dev_f32(c["ks"]), dev_f32(c["vs"]),
+                                    dev_i32(c["tables"]), dev_i32(c["lens"]), c["block"],
+                                    cu_q=None if c["uniform"] else dev_i32(c["cu"]), tree_mask=tree,
+                                    per_tensor=c["per_tensor"]))
+
+
+STREAM, MORE, TILES = ([4], 2, 4), ([40], 2, 4), ([65, 65], 32, 8)
+
+
+# ------------------------------------------------- infinite scales of values
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("place", ["seen by all", "seen by some"])
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("shape,D", [(STREAM, 128), (MORE, 128), (STREAM, 64), (STREAM, 256), (STREAM, 24), (TILES, 128),
+                                     (([40, 40], 32, 4), 64), (([65, 65], 16, 8), 256)])
+def test_an_infinite_value_scale_gives_signed_infinities(shape, D, tree, place, sign):
+    """sum p v sv with sv infinite: the code's sign decides, a code of 0 gives NaN; other rows and heads are untouched."""
+    p = need_gpu()
+    new, H, G = shape
+    n = new[0]
+    say(f"infinite value scale new={new} H={H} G={G} D={D} tree={tree} {place} {sign}")
+    masks = None
+    if tree:
+        parents = np.array([[-1, -1] + [m % 2 for m in range(n - 3)]] * len(new), np.int32)
+        masks = ot.tree_attention_masks(parents)[0]
+    c = paged_case(61, new, [140] * len(new), H, G, D, tree=masks)
+    L = int(c["lens"][0])
+    j = 3 if place == "seen by all" else L - n + 2
+    slot = c["tables"][0, j // 16] * 16 + j % 16
+    c["vc"][slot, 1, 5] = 0x00                           # +0 and -0 among the key's codes
+    c["vc"][slot, 1, 6] = 0x80
+    before = run(p, c)
+    c["vs"][slot, 1] = sign * np.inf
+    out = run(p, c)
+    seen = np.zeros(out.shape[0], bool)
+    seen[:n] = (oa.tree_seen([int(m) for m in masks[0]], L) if tree else oa.chain_seen(n, L))[:, j]
+    assert seen.any() and seen[:n].all() == (place == "seen by all")
+    hit = np.zeros(out.shape, bool)
+    hit[seen, G:2 * G] = True
+    np.testing.assert_array_equal(out[~hit], before[~hit])
+    code = e4m3.decode(c["vc"][slot, 1])
+    want = np.where(code == 0, np.nan, np.copysign(np.inf, code * sign))
+    got = out[seen][:, G:2 * G]
+    np.testing.assert_array_equal(got, np.broadcast_to(want, got.shape))
