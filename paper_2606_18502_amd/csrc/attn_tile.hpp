@@ -94,9 +94,10 @@ struct ValueReads {
 
 // One tile of 64 keys at LDS `kt`, `vt` for a wave's 32 rows.  full: every row sees all of it; otherwise a row
 // sees the keys of `row_sees`.  SCALED: keys and values have scales of their own in LDS, the keys' with c2 in them.
+// odd: c2 is no positive finite number (a tensor's scale of 0, say), and scores take it before unseen ones become -inf.
 template <int DP, bool SCALED>
 __device__ __forceinline__ void attend_tile(RowState<DP>& st, const bf16x8_t (&q)[DP / 16], uint32_t kt, uint32_t vt,
-                                            uint64_t row_sees, bool full, float c2, const float* k_scales,
+                                            uint64_t row_sees, bool full, float c2, bool odd, const float* k_scales,
                                             const float* v_scales) {
     using C = TileShape_<DP>;
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
@@ -126,6 +127,13 @@ __device__ __forceinline__ void attend_tile(RowState<DP>& st, const bf16x8_t (&q
             for (int e = 0; e < 4; ++e)                      // over the reference already: one instruction, not two
                 s[x >> 2][4 * (x & 3) + e] = fmaf(s[x >> 2][4 * (x & 3) + e], f[e], -ref);
         }
+    }
+    if (!SCALED && odd) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[kb][i] *= c2;
+        c2 = 1.0f;
     }
     if (!full) {
         const uint64_t seen = row_sees >> (4 * h);           // bit 32 kb + 8 (i/4) + i % 4: key 4 h further
@@ -446,7 +454,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void prompt_tile_kernel(Pro
         }
         if (k0 <= wave_last)
             attend_tile<DP, false>(st, q, kt, kt + C::kTile, first_keys(i + 1 - k0), k0 + C::kKeys - 1 <= wave_first, c2,
-                                   nullptr, nullptr);
+                                   false, nullptr, nullptr);
         wait_loads<0>();
         __syncthreads();
     }
@@ -519,6 +527,7 @@ __global__ __launch_bounds__(64 * kTileWaves<DP>, DP == 256 ? 1 : 2) void paged_
     const int heads = uniform(a.H);
     const float* const scale_from = tid & 64 ? a.v_scale : a.k_scale;
     const float c2 = a.scale * 1.4426950408889634f * (PT ? a.k_scale[0] : 1.0f);
+    const bool odd_c2 = PT && uniform(!(c2 > 0.0f && c2 < INFINITY));
 
     while (line.next(a, sh)) {
         const int n = line.n, L = line.L, first = line.first, head = line.hg;
@@ -659,7 +668,7 @@ __global__ __launch_bounds__(64 * kTileWaves<DP>, DP == 256 ? 1 : 2) void paged_
             }
             if (k0 <= wave_last) {
                 const bool full = mask == ~0ull && k0 + C::kKeys - 1 <= wave_all;
-                attend_tile<DP, !PT>(st, q, kt, kt + C::kTile, full ? 0 : sees(k0) & mask, full, c2, sc, sc + 64);
+                attend_tile<DP, !PT>(st, q, kt, kt + C::kTile, full ? 0 : sees(k0) & mask, full, c2, odd_c2, sc, sc + 64);
             }
             if (t + 1 < count) write(t + 1);
             __syncthreads();

@@ -64,3 +64,38 @@ def test_an_infinite_value_scale_gives_signed_infinities(shape, D, tree, place, 
     want = np.where(code == 0, np.nan, np.copysign(np.inf, code * sign))
     got = out[seen][:, G:2 * G]
     np.testing.assert_array_equal(got, np.broadcast_to(want, got.shape))
+
+
+# ------------------------------------------------------- scales of a tensor
+
+@pytest.mark.parametrize("shape,D", [(STREAM, 128), (TILES, 128), (([40, 40], 32, 4), 64), (([65, 65], 16, 8), 256), (STREAM, 24)])
+def test_a_key_scale_of_zero_gives_equal_weights(shape, D):
+    """All scores are 0; keys that a row does not see still have no weight."""
+    p = need_gpu()
+    new, H, G = shape
+    say(f"key scale 0 new={new} H={H} G={G} D={D}")
+    c = paged_case(62, new, [70] * len(new), H, G, D, per_tensor=True)
+    c["ks"][:] = 0.0
+    ref, tol = paged_reference(c)
+    assert within(run(p, c), ref, tol) <= 1.0
+
+
+@pytest.mark.parametrize("which", ["ks"])
+@pytest.mark.parametrize("value", [np.nan, np.inf])
+@pytest.mark.parametrize("new,lens,H,G,D", [([4, 4], [2, 40], 2, 4, 128), ([90, 90], [61, 300], 32, 8, 128), ([1100], [1002], 4, 8, 128),
+                                            ([1100], [1002], 4, 8, 64), ([1100], [1002], 4, 8, 256), ([5, 5], [2, 9], 2, 2, 24)])
+def test_rows_that_see_nothing_are_zeros_whatever_the_scales(which, value, new, lens, H, G, D):
+    """More rows than tokens: the first rows see none.  One scale of the tensor that is NaN or infinite reaches the others."""
+    p = need_gpu()
+    say(f"{which} {value} new={new} lens={lens} H={H} G={G} D={D}")
+    c = paged_case(63, new, [max(x - n, 0) for x, n in zip(lens, new)], H, G, D, per_tensor=True)
+    c["lens"] = np.array(lens, np.int32)
+    c[which][:] = value
+    out = run(p, c)
+    first = 0
+    for n, L in zip(new, lens):
+        none = max(n - L, 0)
+        assert (out[first:first + none] == 0).all()
+        if which == "vs" or value != value:              # (infinite scores of both signs: some rows see -inf alone)
+            assert not np.isfinite(out[first + none:first + n]).any()
+        first += n
