@@ -679,13 +679,15 @@ __global__ __launch_bounds__(64 * kTileWaves<DP>, DP == 256 ? 1 : 2) void paged_
             if (there) store_rows(st, a.out + (int64_t)(first + i) * a.ld_out + (int64_t)(head * G + g) * a.D, a.D, v_scale);
         } else {
             const Parts<kThreads, kRows, 1, DP, decltype(line)> parts(line, part, tickets, groups);
+            // (a row that sees none of these keys has sums of 0, also under an infinite or NaN scale)
+            const float part_scale = st.l == 0.0f ? 1.0f : v_scale;
             f32x4_t* const box = reinterpret_cast<f32x4_t*>(tile_smem + w * 32 * DP * 4);
 #pragma unroll
             for (int d = 0; d < C::DB; ++d)
 #pragma unroll
                 for (int x = 0; x < 4; ++x)
                     box[RowBox<DP>::at(l32, 8 * d + 2 * x + h)] =
-                        f32x4_t{st.o[d][4 * x], st.o[d][4 * x + 1], st.o[d][4 * x + 2], st.o[d][4 * x + 3]} * v_scale;
+                        f32x4_t{st.o[d][4 * x], st.o[d][4 * x + 1], st.o[d][4 * x + 2], st.o[d][4 * x + 3]} * part_scale;
             RowBox<DP>::store_part(box, parts.sums(parts.me) + 32 * w * DP,
                                       (int)max(min(R - row0 - 32 * w, (int64_t)32), (int64_t)0));
             if (there && h == 0) parts.store_ml(32 * w + l32, st.m, st.l);

@@ -80,7 +80,7 @@ def test_a_key_scale_of_zero_gives_equal_weights(shape, D):
     assert within(run(p, c), ref, tol) <= 1.0
 
 
-@pytest.mark.parametrize("which", ["ks"])
+@pytest.mark.parametrize("which", ["ks", "vs"])
 @pytest.mark.parametrize("value", [np.nan, np.inf])
 @pytest.mark.parametrize("new,lens,H,G,D", [([4, 4], [2, 40], 2, 4, 128), ([90, 90], [61, 300], 32, 8, 128), ([1100], [1002], 4, 8, 128),
                                             ([1100], [1002], 4, 8, 64), ([1100], [1002], 4, 8, 256), ([5, 5], [2, 9], 2, 2, 24)])
