@@ -278,10 +278,11 @@ struct Parts {
                 const int d = from[k] - at_row[k] * DP;
                 if (output) {
                     const int h = at_row[k] / ROWS, row = l.rt * ROWS + at_row[k] % ROWS, i = row / G, g = row - i * G;
-                    const float f = sum[k] == 0.0f ? 0.0f : 1.0f / sum[k];
+                    const bool none = sum[k] == 0.0f;
+                    const float f = 1.0f / sum[k];
                     uint2 y;
-                    y.x = f32_to_bf16x2(acc[k][0] * f, acc[k][1] * f);
-                    y.y = f32_to_bf16x2(acc[k][2] * f, acc[k][3] * f);
+                    y.x = none ? 0 : f32_to_bf16x2(acc[k][0] * f, acc[k][1] * f);
+                    y.y = none ? 0 : f32_to_bf16x2(acc[k][2] * f, acc[k][3] * f);
                     *reinterpret_cast<uint2*>(a.out + (int64_t)(l.first + i) * a.ld_out +
                                               (int64_t)((l.hg * HG + h) * G + g) * a.D + d) = y;
                 } else {

@@ -468,14 +468,15 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
         const auto store_rows = [&](int x, int h, float total_l, const f32x4_t (&v)[NB]) {
             const int row = rt * C::kRows + x * 16 + q16, i = row / G, g = row - i * G;
             if (row >= R) return;
-            const float inv = total_l == 0.0f ? 0.0f : 1.0f / total_l;
+            const bool none = total_l == 0.0f;               // (zeros, whatever the values that had no weight)
+            const float inv = 1.0f / total_l;
             uint16_t* const dst = a.out + (int64_t)(first + i) * a.ld_out + (int64_t)(h * G + g) * a.D + 4 * qd;
 #pragma unroll
             for (int d = 0; d < NB; ++d) {
                 if (16 * d < a.D) {
                     uint2 y;
-                    y.x = f32_to_bf16x2(v[d][0] * inv, v[d][1] * inv);
-                    y.y = f32_to_bf16x2(v[d][2] * inv, v[d][3] * inv);
+                    y.x = none ? 0 : f32_to_bf16x2(v[d][0] * inv, v[d][1] * inv);
+                    y.y = none ? 0 : f32_to_bf16x2(v[d][2] * inv, v[d][3] * inv);
                     *reinterpret_cast<uint2*>(dst + 16 * d) = y;
                 }
             }

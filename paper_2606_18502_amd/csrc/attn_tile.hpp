@@ -334,7 +334,8 @@ __device__ __forceinline__ void end_rows(RowState<DP>& st) {
 // The rows' results as bf16: channels 32 d + 8 x + 4 (lane/32) .. of this lane's row, `dst` its first channel.
 template <int DP>
 __device__ __forceinline__ void store_rows(const RowState<DP>& st, uint16_t* dst, int D, float scale) {
-    const float inv = st.l == 0.0f ? 0.0f : scale / st.l;
+    const bool none = st.l == 0.0f;                          // (zeros, whatever the values that had no weight)
+    const float inv = scale / st.l;
     dst += 4 * ((threadIdx.x >> 5) & 1);
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
@@ -342,8 +343,8 @@ __device__ __forceinline__ void store_rows(const RowState<DP>& st, uint16_t* dst
         for (int x = 0; x < 4; ++x)
             if (32 * d + 8 * x < D) {
                 uint2 y;
-                y.x = f32_to_bf16x2(st.o[d][4 * x] * inv, st.o[d][4 * x + 1] * inv);
-                y.y = f32_to_bf16x2(st.o[d][4 * x + 2] * inv, st.o[d][4 * x + 3] * inv);
+                y.x = none ? 0 : f32_to_bf16x2(st.o[d][4 * x] * inv, st.o[d][4 * x + 1] * inv);
+                y.y = none ? 0 : f32_to_bf16x2(st.o[d][4 * x + 2] * inv, st.o[d][4 * x + 3] * inv);
                 *reinterpret_cast<uint2*>(dst + 32 * d + 8 * x) = y;
             }
 }

@@ -99,3 +99,48 @@ def test_rows_that_see_nothing_are_zeros_whatever_the_scales(which, value, new, 
         if which == "vs" or value != value:              # (infinite scores of both signs: some rows see -inf alone)
             assert not np.isfinite(out[first + none:first + n]).any()
         first += n
+
+
+# ---------------------------------------------------- scores of -inf, prompts
+
+def prompt(p, q, k, v, lens):
+    cu = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    d = [dev_bf16(wl.bf16_bits_from_f32(x.astype(np.float32))) for x in (q, k, v)]
+    return values(p.prompt_attention(*d, dev_i32(cu)))
+
+
+@pytest.mark.parametrize("value", [np.inf, np.nan])
+@pytest.mark.parametrize("D", [128, 64, 256])
+@pytest.mark.parametrize("n", [20, 200])
+def test_rows_of_scores_of_minus_infinity_alone_are_zeros_whatever_the_values(D, value, n):
+    """The first two tokens' keys give -inf to every query; the first one's value is infinite or NaN."""
+    p = need_gpu()
+    rng = np.random.default_rng(65)
+    q = np.abs(rng.standard_normal((n, 2, D))) + 0.25
+    k, v = rng.standard_normal((n, 1, D)), rng.standard_normal((n, 1, D))
+    k[:2, 0, 1] = -np.inf
+    v[0, 0, 5] = value
+    out = prompt(p, q, k, v, [n])
+    assert (out[:2] == 0).all()
+    assert np.isfinite(np.delete(out, 5, axis=2)).all()
+
+
+@pytest.mark.parametrize("shape,D", [(STREAM, 128), (MORE, 128), (STREAM, 64), (STREAM, 256), (STREAM, 24), (TILES, 128),
+                                     (([40, 40], 32, 4), 64), (([65, 65], 16, 8), 256)])
+@pytest.mark.parametrize("value", [np.inf, np.nan])
+def test_paged_rows_of_scores_of_minus_infinity_alone_are_zeros(shape, D, value):
+    """The first two tokens have an infinite key scale and keys below 0, queries above; the first one's value scale is
+    infinite or NaN."""
+    p = need_gpu()
+    new, H, G = shape
+    c = paged_case(66, new, [0] * len(new), H, G, D)
+    q = np.abs(c["q"]) + 0.25
+    c["q_bits"] = wl.bf16_bits_from_f32(q.astype(np.float32))
+    for j in range(2):
+        slot = c["tables"][0, 0] * 16 + j
+        c["kc"][slot, 1] = 0xB8                          # -1
+        c["ks"][slot, 1] = np.inf
+    c["vs"][c["tables"][0, 0] * 16, 1] = value
+    out = run(p, c)
+    assert (out[:2, G:2 * G] == 0).all()
+    assert np.isfinite(out[:, :G]).all() and np.isfinite(out[new[0]:]).all()
