@@ -410,12 +410,21 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void prompt_tile_kernel(Pro
     for (int x = 0; x < C::kLoads; ++x) {
         const int r = (4 * x + w) * kPer + ld_key;
         const int ck = ld_slot ^ tile_k_swizzle<DP>(r), cv = ld_slot ^ tile_v_swizzle<DP>(r);
-        k_part[x] = ck < chunks ? ck * 8 : 0;                                  // (past the head's end: any; queries are 0)
-        v_part[x] = cv < chunks ? cv * 8 : 0;
+        k_part[x] = ck < chunks ? ck * 8 : -1;                                 // (past the head's end: not loaded, 0)
+        v_part[x] = cv < chunks ? cv * 8 : 0;                                  // (past the head's end: any, not stored)
         k_at[x] = k_rows + r * a.ld_k + k_part[x];
         v_at[x] = v_rows + r * a.ld_v + v_part[x];
     }
     const int64_t k_step = C::kKeys * a.ld_k, v_step = C::kKeys * a.ld_v;
+    // Keys' columns past the head's end stay 0: a key's infinity there times the queries' 0 would be NaN.
+    const bool whole = a.D == DP;
+    if (!whole) {
+        for (int x = tid * 16; x < C::kTile; x += 256 * 16) {
+            *reinterpret_cast<u32x4_t*>(tile_smem + x) = u32x4_t{0, 0, 0, 0};
+            *reinterpret_cast<u32x4_t*>(tile_smem + 2 * C::kTile + x) = u32x4_t{0, 0, 0, 0};
+        }
+        __syncthreads();
+    }
     const auto stage = [&](int t) {
         const uint32_t to = smem + (t & 1) * 2 * C::kTile;
         if ((t + 1) * C::kKeys > n) {                                          // past the end: the last key again
@@ -428,7 +437,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void prompt_tile_kernel(Pro
         }
 #pragma unroll
         for (int x = 0; x < C::kLoads; ++x) {
-            load_lds16(k_at[x], to + (4 * x + w) * 1024);
+            if (whole || k_part[x] >= 0) load_lds16(k_at[x], to + (4 * x + w) * 1024);
             load_lds16(v_at[x], to + C::kTile + (4 * x + w) * 1024);
             k_at[x] += k_step;
             v_at[x] += v_step;

@@ -109,8 +109,40 @@ def prompt(p, q, k, v, lens):
     return values(p.prompt_attention(*d, dev_i32(cu)))
 
 
+@pytest.mark.parametrize("D", [128, 96, 80, 72, 64, 40, 8, 256, 200, 136])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("n,j", [(150, 3), (150, 100), (20, 0), (20, 7)])
+def test_an_infinite_key_element_decides_by_the_query_sign(D, sign, n, j):
+    """A score of -inf has no weight (a row with no other is zeros), one of +inf gives NaN: the same for heads that fill
+    their tile's columns and for heads that do not."""
+    p = need_gpu()
+    H, G = 2, 2
+    say(f"infinite key element D={D} sign={sign} n={n} j={j}")
+    rng = np.random.default_rng(64 + D)
+    r = lambda h: wl.f32_from_bf16_bits(wl.bf16_bits_from_f32(rng.standard_normal((n, h, D)).astype(np.float32))).astype(np.float64)
+    q, k, v = r(H * G), r(H), r(H)
+    ch = 3 % D
+    q[:, :, ch] = np.where(np.abs(q[:, :, ch]) < 0.25, 0.25, q[:, :, ch])         # (no 0 * inf)
+    plain = oa.attention(q, k, v, oa.chain_seen(n, n), D ** -0.5)
+    hidden = oa.chain_seen(n, n)
+    hidden[:, j] = False
+    without, spread, mag = oa.attention(q, k, v, hidden, D ** -0.5)
+    k[j, 1, ch] = sign * np.inf
+    out = prompt(p, q, k, v, [n])
+    tol = oa.bound(*plain, D, n)
+    assert within(out[:, :G], plain[0][:, :G], tol[:, :G]) <= 1.0                # the other KV head
+    assert within(out[:j, G:], plain[0][:j, G:], tol[:j, G:]) <= 1.0             # earlier rows
+    up = (np.sign(q[j:, G:, ch]) * sign) > 0
+    assert np.isnan(out[j:, G:][up]).all()
+    tol = oa.bound(without, spread, mag, D, n)
+    got, ref, t = out[j:, G:][~up], without[j:, G:][~up], tol[j:, G:][~up]
+    assert within(got, ref, t) <= 1.0
+    if j == 0:
+        assert (out[0, G:][~up[0]] == 0).all()
+
+
 @pytest.mark.parametrize("value", [np.inf, np.nan])
-@pytest.mark.parametrize("D", [128, 64, 256])
+@pytest.mark.parametrize("D", [128, 64, 256, 96])
 @pytest.mark.parametrize("n", [20, 200])
 def test_rows_of_scores_of_minus_infinity_alone_are_zeros_whatever_the_values(D, value, n):
     """The first two tokens' keys give -inf to every query; the first one's value is infinite or NaN."""
