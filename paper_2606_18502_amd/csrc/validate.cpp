@@ -13,7 +13,7 @@ inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 
 
 constexpr int64_t kMaxGrid = 2147483647;   // grid.x limit
 constexpr int64_t kMaxGridY = 65535;       // grid.y limit
-constexpr int64_t kMaxTokens = kMaxGrid - 65535;   // of a sequence: positions a few tiles further still fit
+constexpr int64_t kMaxTokens = kMaxGrid - 65535;   // of a sequence, and sequences: positions a few tiles further still fit
 
 }  // namespace
 
@@ -88,7 +88,7 @@ namespace {
 spec_status check_heads(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D, float scale) {
     if (T < 0 || B < 0 || Hq <= 0 || H <= 0 || D <= 0 || Hq % H != 0) return SPEC_ERR_SHAPE;
     if (D % 8 != 0 || D > 256) return SPEC_ERR_UNSUPPORTED;
-    if (Hq > kMaxGridY || T > kMaxGrid / Hq || B > kMaxGrid) return SPEC_ERR_UNSUPPORTED;
+    if (Hq > kMaxGridY || T > kMaxGrid / Hq || B > kMaxTokens) return SPEC_ERR_UNSUPPORTED;
     if (!isfinite(scale) || !(scale > 0.0f)) return SPEC_ERR_VALUE;
     return SPEC_OK;
 }
