@@ -534,8 +534,8 @@ spec_status spec_fp8_kv_cache_read(const uint8_t* k_cache, const uint8_t* v_cach
  * D <= 256, Hq <= 65535, T*Hq and num_blocks < 2^31, B and max_blocks*block_size < 2^31 - 65535,
  * block_size*H*D < 2^32 (SPEC_ERR_UNSUPPORTED); q, out,
  * k_cache and v_cache 16-byte aligned, ld_q and ld_out multiples of 8, tree_mask 8-byte, the
- * tables, lengths and scales 4-byte aligned (SPEC_ERR_ALIGN); scale finite and > 0
- * (SPEC_ERR_VALUE); mode PER_ROW or PER_TENSOR (SPEC_ERR_ENUM).
+ * tables, lengths and scales 4-byte aligned (SPEC_ERR_ALIGN); scale > 0 and
+ * fl32(scale*log2(e)) finite (SPEC_ERR_VALUE); mode PER_ROW or PER_TENSOR (SPEC_ERR_ENUM).
  */
 size_t spec_fp8_paged_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D);
 
@@ -562,7 +562,8 @@ spec_status spec_fp8_paged_attention(const void* q, int64_t ld_q, const uint8_t*
  * Requirements: T, B >= 0 (0: no-op), Hq, H, D > 0, Hq % H == 0, ld_q, ld_out >= Hq*D, ld_k,
  * ld_v >= H*D (SPEC_ERR_SHAPE); D % 8 == 0, D <= 256, Hq <= 65535, T*Hq < 2^31,
  * (T*Hq/H/128 + B)*H < 2^24 (SPEC_ERR_UNSUPPORTED); all tensors 16-byte aligned with strides
- * that are multiples of 8, cu_seqlens 4-byte aligned (SPEC_ERR_ALIGN); scale finite and > 0 (SPEC_ERR_VALUE).  No workspace.
+ * that are multiples of 8, cu_seqlens 4-byte aligned (SPEC_ERR_ALIGN); scale > 0 and
+ * fl32(scale*log2(e)) finite (SPEC_ERR_VALUE).  No workspace.
  */
 spec_status spec_prompt_attention_bf16(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v,
                                        int64_t ld_v, const int32_t* cu_seqlens, int64_t T, int64_t B, int64_t Hq,

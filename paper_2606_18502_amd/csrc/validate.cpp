@@ -89,7 +89,7 @@ spec_status check_heads(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D, 
     if (T < 0 || B < 0 || Hq <= 0 || H <= 0 || D <= 0 || Hq % H != 0) return SPEC_ERR_SHAPE;
     if (D % 8 != 0 || D > 256) return SPEC_ERR_UNSUPPORTED;
     if (Hq > kMaxGridY || T > kMaxGrid / Hq || B > kMaxTokens) return SPEC_ERR_UNSUPPORTED;
-    if (!isfinite(scale) || !(scale > 0.0f)) return SPEC_ERR_VALUE;
+    if (!(scale > 0.0f) || !isfinite(scale * 1.4426950408889634f)) return SPEC_ERR_VALUE;
     return SPEC_OK;
 }
 

@@ -45,3 +45,13 @@ def test_sequences_leave_room_for_the_kernels_arithmetic(lib):
     assert paged(lib, B=top) == HIP
     for B in (top + 1, 2 ** 31 - 255, 2 ** 31 - 1):
         assert paged(lib, B=B) == UNSUP, B
+
+
+def test_a_softmax_scale_whose_powers_of_two_overflow_is_refused(lib):
+    """Scores are taken to base 2: scale * log2(e) has to be finite in fp32, or a score of 0 would be 0 * inf."""
+    for f in (lambda s: paged(lib, scale=s), lambda s: prompt(lib, scale=s)):
+        assert f(2.0 ** 126) == HIP
+        assert f(2.0 ** -149) == HIP
+        assert f(2.0 ** 127) == HIP                      # 2^127 log2(e) = 1.4427 * 2^127 < 2^128
+        assert f(1.5 * 2.0 ** 127) == VALUE              # 2.16 * 2^127
+        assert f(3.4e38) == VALUE
