@@ -509,8 +509,10 @@ spec_status spec_fp8_kv_cache_read(const uint8_t* k_cache, const uint8_t* v_cach
  * included.  An infinite scale of a value seen gives infinities of its codes' signs, NaN where
  * the code is 0.  Products of q and codes are exact; they are summed, and the sums
  * of p and p*v accumulated, in fp32; p_ij * sv_j (or p_ij alone, where one
- * scale holds for the tensor) enters the second product as bf16: as the sum of two for few
- * rows, rounded to nearest for many.
+ * scale holds for the tensor) enters the second product in bf16: for few rows as the sum of
+ * two (off by 2^-15 of its term at most), for many rounded once (2^-8), but for rows that
+ * see at most 64 tokens as two there, too (2^-16).  Which a call takes depends on the rows of an average
+ * sequence, T/B * Hq/H, on H and on D (many: 80 to 257 or more).
  *
  * q        bf16 [T, ld_q], head h at columns [h*D, (h+1)*D).  The rows of sequence b are
  *          cu_q[b] .. cu_q[b+1]-1, or with cu_q NULL T/B rows each (T % B == 0,
@@ -551,7 +553,8 @@ spec_status spec_fp8_paged_attention(const void* q, int64_t ld_q, const uint8_t*
  * spec_prompt_attention_bf16 -- causal attention over B whole prompts packed
  * one after the other (the prefill that fills the cache): row i of a prompt
  * sees its rows 0..i.  Scores, reference and sums as spec_fp8_paged_attention,
- * with bf16 keys and values and p_ij rounded to bf16 for the second product.
+ * with bf16 keys and values; for the second product p_ij is rounded to bf16 (2^-8 of its term
+ * at most), in rows that see at most 64 tokens to the sum of two (2^-16).
  *
  * q  bf16 [T, ld_q], Hq heads of D; k, v bf16 [T, ld_k] / [T, ld_v], H heads of D: the column
  *    blocks of the QKV projection's output fit directly.  Query head g reads KV head g / (Hq/H).

@@ -1,7 +1,7 @@
 // Attention of many rows (whole prompts, long chunks): tiles on the matrix cores.
 //
 // Mathematics: as in attn_stream.hpp (a running reference that moves only when
-// a score exceeds it by 2^8; p rounded to bf16 for the second product; sums in
+// a score exceeds it by 2^8; p rounded to bf16 for the second product, to two in rows of few keys; sums in
 // fp32).
 //
 // A workgroup of 4 waves owns 128 rows -- a row is a (token, query head) pair, the
@@ -56,6 +56,10 @@ __device__ __forceinline__ int tile_v_swizzle(int r) {
     else return (r & 3) << 2;
 }
 
+// Rows of tiles whose first row sees at most this many keys keep their weights to 16 bits, as few rows do: a weight's
+// rounding is most of the error of a row of few keys, and the same one in all its channels.  One tile of keys: prompts
+// of 1..130 tokens take 9.0 us as before (128: 10.8), one of 8191 538 (531).  For every row: 848 us, nine prompts 236 (158).
+constexpr int kFewKeys = 64;
 // What a wave keeps of its 32 rows.
 template <int DP>
 struct RowState {
@@ -95,10 +99,12 @@ struct ValueReads {
 // One tile of 64 keys at LDS `kt`, `vt` for a wave's 32 rows.  full: every row sees all of it; otherwise a row
 // sees the keys of `row_sees`.  SCALED: keys and values have scales of their own in LDS, the keys' with c2 in them.
 // odd: c2 is no positive finite number (a tensor's scale of 0, say), and scores take it before unseen ones become -inf.
+// both: weights enter the second product as two bf16, each rounded and what that leaves (in a pass of its own: in the
+// first one, before its products, it takes the registers of the tiles that do without).
 template <int DP, bool SCALED>
 __device__ __forceinline__ void attend_tile(RowState<DP>& st, const bf16x8_t (&q)[DP / 16], uint32_t kt, uint32_t vt,
-                                            uint64_t row_sees, bool full, float c2, bool odd, const float* k_scales,
-                                            const float* v_scales) {
+                                            uint64_t row_sees, bool full, float c2, bool odd, bool both,
+                                            const float* k_scales, const float* v_scales) {
     using C = TileShape_<DP>;
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
     // ---- scores
@@ -169,30 +175,34 @@ __device__ __forceinline__ void attend_tile(RowState<DP>& st, const bf16x8_t (&q
 #pragma unroll
         for (int d = 0; d < C::DB; ++d) st.o[d] *= down;
     }
-    // ---- probabilities
-    bf16x8_t p[4];
+    // ---- probabilities: two at a time, those of element i of step u
     float sum = 0.0f;
+    const auto weights = [&](int u, int e) -> float2 {
+        const int i = 8 * (u & 1) + 2 * e;
+        float a, b;
+        if constexpr (SCALED) {
+            a = exp2_hw(s[u >> 1][i]);
+            b = exp2_hw(s[u >> 1][i + 1]);
+        } else {
+            a = exp2_hw(fmaf(s[u >> 1][i], c2, -st.m));
+            b = exp2_hw(fmaf(s[u >> 1][i + 1], c2, -st.m));
+        }
+        sum += a + b;
+        if constexpr (SCALED) {
+            const float2 f = *reinterpret_cast<const float2*>(v_scales + 16 * u + 8 * (e >> 1) + 4 * h + 2 * (e & 1));
+            a *= f.x;
+            b *= f.y;
+        }
+        return float2{a, b};
+    };
+    bf16x8_t p[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
         u32x4_t w;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int i = 8 * (u & 1) + 2 * e;
-            float a, b;
-            if constexpr (SCALED) {
-                a = exp2_hw(s[u >> 1][i]);
-                b = exp2_hw(s[u >> 1][i + 1]);
-            } else {
-                a = exp2_hw(fmaf(s[u >> 1][i], c2, -st.m));
-                b = exp2_hw(fmaf(s[u >> 1][i + 1], c2, -st.m));
-            }
-            sum += a + b;
-            if constexpr (SCALED) {
-                const float2 f = *reinterpret_cast<const float2*>(v_scales + 16 * u + 8 * (e >> 1) + 4 * h + 2 * (e & 1));
-                a *= f.x;
-                b *= f.y;
-            }
-            w[e] = f32_to_bf16x2(a, b);
+            const float2 x = weights(u, e);
+            w[e] = f32_to_bf16x2(x.x, x.y);
         }
         p[u] = __builtin_bit_cast(bf16x8_t, w);
     }
@@ -205,6 +215,24 @@ __device__ __forceinline__ void attend_tile(RowState<DP>& st, const bf16x8_t (&q
         for (int d = 0; d < C::DB; ++d)
             st.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, values(u, d)), p[u], st.o[d],
                                                               0, 0, 0);
+    if (__builtin_expect(both, false)) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            u32x4_t w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float2 x = weights(u, e);
+                const uint32_t up = f32_to_bf16x2(x.x, x.y);
+                // (an infinite weight is its upper half alone: inf - inf is NaN)
+                w[e] = f32_to_bf16x2(fabsf(x.x) < INFINITY ? x.x - __uint_as_float(up << 16) : 0.0f,
+                                     fabsf(x.y) < INFINITY ? x.y - __uint_as_float(up & 0xffff0000u) : 0.0f);
+            }
+#pragma unroll
+            for (int d = 0; d < C::DB; ++d)
+                st.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, values(u, d)),
+                                                                  __builtin_bit_cast(bf16x8_t, w), st.o[d], 0, 0, 0);
+        }
+    }
 }
 
 // An infinite or NaN value reaches the rows that see its key and no others (0 * inf is NaN): in a tile that
@@ -451,12 +479,13 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void prompt_tile_kernel(Pro
     for (int ks = 0; ks < C::KS; ++ks) asm volatile("" : "+v"(q[ks]));
     __syncthreads();
     const float c2 = a.scale * 1.4426950408889634f;
+    const bool both = first_token < kFewKeys;
     for (int t = 0; t < tiles; ++t) {
         if (t + 1 < tiles) stage(t + 1);
         const uint32_t kt = smem + (t & 1) * 2 * C::kTile;
         const int k0 = t * C::kKeys;
         uint8_t* const values = tile_smem + (t & 1) * 2 * C::kTile + C::kTile;
-        if (k0 + C::kKeys - 1 > first_token && __syncthreads_or(wild_part<DP>(values))) {
+        if ((both || k0 + C::kKeys - 1 > first_token) && __syncthreads_or(wild_part<DP>(values))) {
             mark_tile(st, kt + C::kTile, first_keys(i + 1 - k0));
             __syncthreads();
             clean_part<DP>(values);
@@ -464,7 +493,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void prompt_tile_kernel(Pro
         }
         if (k0 <= wave_last)
             attend_tile<DP, false>(st, q, kt, kt + C::kTile, first_keys(i + 1 - k0), k0 + C::kKeys - 1 <= wave_first, c2,
-                                   false, nullptr, nullptr);
+                                   false, both, nullptr, nullptr);
         wait_loads<0>();
         __syncthreads();
     }
@@ -643,6 +672,7 @@ __global__ __launch_bounds__(64 * kTileWaves<DP>, DP == 256 ? 1 : 2) void paged_
                 if (tid < 128) scales[(t & 1) * 128 + tid] = scale_there ? (tid < 64 ? scale * c2 : scale) : 0.0f;
         };
 
+        const bool both = all_see < kFewKeys;
         RowState<DP> st;
         begin_rows(st);
         if (count > 0) {
@@ -678,7 +708,7 @@ __global__ __launch_bounds__(64 * kTileWaves<DP>, DP == 256 ? 1 : 2) void paged_
             }
             if (k0 <= wave_last) {
                 const bool full = mask == ~0ull && k0 + C::kKeys - 1 <= wave_all;
-                attend_tile<DP, !PT>(st, q, kt, kt + C::kTile, full ? 0 : sees(k0) & mask, full, c2, odd_c2, sc, sc + 64);
+                attend_tile<DP, !PT>(st, q, kt, kt + C::kTile, full ? 0 : sees(k0) & mask, full, c2, odd_c2, both, sc, sc + 64);
             }
             if (t + 1 < count) write(t + 1);
             __syncthreads();
