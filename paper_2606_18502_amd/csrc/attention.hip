@@ -159,11 +159,11 @@ int workgroups(const PagedPlan& p, int64_t units, int64_t cells) {
 
 template <int DP, int NQ, int HG>
 hipError_t launch_stream(const PagedPlan& p, const PagedArgs& a, void* workspace, hipStream_t stream) {
-    using C = StreamShape<DP, NQ, HG, 2, 4>;
+    using C = StreamShape<DP, NQ, HG>;
     const int64_t units = ((int64_t)a.T * (a.Hq / a.H) / C::kRows + a.B) * ((a.H + HG - 1) / HG);
     const int grid = workgroups(p, units, std::max<int64_t>(((a.max_len + C::kStep - 1) / C::kStep + 1) / kStreamCell, 1));
     float* const part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(workspace) + kAttnTicketBytes);
-    hipLaunchKernelGGL((paged_stream_kernel<DP, NQ, HG, 2, 4>), dim3(grid), dim3(256), C::kLds, stream, a, part,
+    hipLaunchKernelGGL((paged_stream_kernel<DP, NQ, HG>), dim3(grid), dim3(64 * kStreamWaves), C::kLds, stream, a, part,
                        reinterpret_cast<unsigned int*>(workspace), grid, C::KW == 1 ? 5 : 3);
     return hipGetLastError();
 }

@@ -11,7 +11,7 @@
 // A wave owns one KV head and every KW-th tile of 32 keys, for all rows of the unit:
 // no data is shared between waves, so nothing waits at a barrier until the
 // end of a unit.  Codes go from HBM to LDS without registers (16 bytes per
-// lane from its key's page) into a ring of S stages; table entries of the tile
+// lane from its key's page) into a ring of two stages; table entries of the tile
 // after next travel the same way.
 //   S^T = K Q^T  on v_mfma_f32_16x16x32_bf16: codes are exact in bf16.  A lane holds
 //     the scores of one row (lane % 16) at keys 4 (lane/16) + 0..3 and 16 more.
@@ -56,38 +56,39 @@ __device__ __forceinline__ int v_swizzle(int r) {
 
 constexpr int kStreamCell = 3;                               // steps that are worth a join (1, 2, 4: slower on short lines)
 
-template <int DP, int NQ, int HG, int S, int W>
+constexpr int kStreamWaves = 4;                              // of a workgroup
+
+template <int DP, int NQ, int HG>
 struct StreamShape {
-    static constexpr int KW = W / HG;             // waves that share a head
+    static constexpr int KW = kStreamWaves / HG;             // waves that share a head
     static constexpr int kRows = 16 * NQ;
     static constexpr int kStep = 32 * KW;                    // keys of a step
     static constexpr int kTile = 32 * DP;                    // bytes of a tile's K (V) codes
     static constexpr int kStage = 2 * kTile + 256;           // and 64 scales
-    static constexpr int kTables = S * kStage;               // two tiles' table entries
-    static constexpr int kOffs = kTables + S * 256;          // byte offsets of a tile's rows
+    static constexpr int kTables = 2 * kStage;               // two tiles' table entries
+    static constexpr int kOffs = kTables + 2 * 256;          // byte offsets of a tile's rows
     static constexpr int kWave = (kOffs + 256 + DP - 1) / DP * DP;
-    static constexpr int kLds = W * kWave;
-    static constexpr int kData = DP / 16 + 1;                // loads of a stage
+    static constexpr int kLds = kStreamWaves * kWave;
     static constexpr int kBlocks = DP / 16;
-    static_assert(S >= 2 && S <= 4 && (S - 2) * (kData + 1) < 64, "the waits below count these");
     static_assert(kStage % DP == 0 && kWave % DP == 0, "a V row's address has no bits where its chunks' are");
-    static_assert(KW == 1 || W / 2 * NQ * (kBlocks * 256 + 128) * 4 <= kLds, "half the waves' results fit for the join");
+    static_assert(KW == 1 || kStreamWaves / 2 * NQ * (kBlocks * 256 + 128) * 4 <= kLds, "half the waves' results fit for the join");
 };
 
-template <int DP, int NQ, int HG, int S, int W>
-__global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel(PagedArgs a, float* part, unsigned int* tickets,
-                                                                      int groups, int extra) {
-    using C = StreamShape<DP, NQ, HG, S, W>;
+template <int DP, int NQ, int HG>
+__global__ __launch_bounds__(64 * kStreamWaves, DP == 256 ? 1 : 2) void paged_stream_kernel(PagedArgs a, float* part,
+                                                                                 unsigned int* tickets, int groups, int extra) {
+    using C = StreamShape<DP, NQ, HG>;
+    constexpr int kThreads = 64 * kStreamWaves;
     constexpr int NB = C::kBlocks, KS = DP / 64;
     // (sized at the launch: with the size in its view the compiler counts on one workgroup per CU, and then keeps the
     // sums in AGPRs and copies them for every rescale)
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
-    __shared__ LineShared<64 * W> sh;
+    __shared__ LineShared<kThreads> sh;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int G = a.Hq / a.H;
     const int q16 = lane & 15, qd = lane >> 4;
 
-    Line<64 * W, C::kRows, C::kStep, kStreamCell> line;
+    Line<kThreads, C::kRows, C::kStep, kStreamCell> line;
     if (!line.begin(a, sh, HG, groups, extra)) return;
 
     // ---- this wave's corner of LDS
@@ -158,7 +159,7 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
             const int first_key = 32 * (s_in * C::KW + kw);
             int blk = (first_key + key) / bs, off_t = (first_key + key) - blk * bs, off_p = off_t;
             const auto load_table = [&](int t) {
-                load_lds4(table + min(blk, last_block), ring_at + C::kTables + (t % S) * 256);
+                load_lds4(table + min(blk, last_block), ring_at + C::kTables + (t & 1) * 256);
                 off_t += step_r;
                 blk += step_q;
                 if (off_t >= bs) {
@@ -168,19 +169,19 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
             };
             int next_key = first_key;
             const auto prepare = [&](int t) -> uint32_t {            // byte offsets and scales of tile t; which keys there are
-                const int page = (int)tab[(t % S) * 64 + lane];
+                const int page = (int)tab[(t & 1) * 64 + lane];
                 const bool there = (next_key + key < L) & ((uint32_t)page < num_blocks);
                 const uint32_t pg = there ? page : 0, in = (there ? off_p : 0) * heads + head;
                 const uint64_t row = (uint64_t)pg * page_rows + in;
                 if (lane < 32) offs[key] = (int64_t)((uint64_t)pg * page_bytes + in * head_size);
-                load_lds4(scales + (per_tensor ? 0 : row), ring_at + (t % S) * C::kStage + 2 * C::kTile);
+                load_lds4(scales + (per_tensor ? 0 : row), ring_at + (t & 1) * C::kStage + 2 * C::kTile);
                 off_p += step_r;
                 if (off_p >= bs) off_p -= bs;
                 next_key += C::kStep;
                 return (uint32_t)__ballot(there);
             };
             const auto load_codes = [&](int t) {
-                const uint32_t to = ring_at + (t % S) * C::kStage;
+                const uint32_t to = ring_at + (t & 1) * C::kStage;
 #pragma unroll
                 for (int x = 0; x < C::kTile / 1024; ++x) {
                     const int r = x * kKeys + ld_key;
@@ -191,20 +192,15 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
                     load_lds16(a.v_cache + at_row + (cv < chunks ? cv * 16 : 0), to + C::kTile + x * 1024);
                 }
             };
-            // A tile's group of loads: its scales, the table entries of the tile S - 1 later, its codes.  In order, so
-            // that a tile's codes are there when its group's count is, and the table entries that the next group
-            // needs with them.
-            uint32_t th[S];
+            // A tile's group of loads: its scales, the table entries that the next group needs, its codes.
             const auto load_group = [&](int t) -> uint32_t {
                 const uint32_t there = prepare(t);
-                if (t + S - 1 < count) load_table(t + S - 1);
+                if (t + 1 < count) load_table(t + 1);
                 load_codes(t);
                 return there;
             };
             wait_lds();
-#pragma unroll
-            for (int t = 0; t < S - 1; ++t)
-                if (t < count) load_table(t);
+            load_table(0);
             wait_loads<0>();
             // (the queries, too: a wait for them in the loop would drain the ring)
 #pragma unroll
@@ -213,16 +209,12 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
                 for (int s = 0; s < KS; ++s)
 #pragma unroll
                     for (int u = 0; u < 2; ++u) asm volatile("" : "+v"(q[x][s][u]));
-#pragma unroll
-            for (int t = 0; t < S - 1; ++t) {
-                th[t] = 0;
-                if (t < count) th[t] = load_group(t);
-            }
+            uint32_t there = load_group(0);
 
             // One tile; full: every row sees every key of it.
             const auto attend = [&](int t, int k0, uint32_t there, bool full) {
-                const uint32_t stage = ring_at + (t % S) * C::kStage;
-                const uint8_t* const kt = ring + (t % S) * C::kStage;
+                const uint32_t stage = ring_at + (t & 1) * C::kStage;
+                const uint8_t* const kt = ring + (t & 1) * C::kStage;
                 const float* const sc = reinterpret_cast<const float*>(kt + 2 * C::kTile);
 
                 // ---- scores
@@ -399,19 +391,13 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
             };
 
             for (int t = 0; t < count; ++t) {
-                // codes of t: the groups behind it are those of t+1 .. t+S-2
-                const int behind = min(S - 2, count - 1 - t);
-                if (t + 2 * S - 3 < count) wait_loads<(S - 2) * (C::kData + 1)>();
-                else if (S > 3 && behind == 2) wait_loads<(S > 3 ? 2 : 0) * C::kData>();
-                else if (S > 2 && behind >= 1) wait_loads<(S > 2 ? 1 : 0) * C::kData>();
-                else wait_loads<0>();
+                wait_loads<0>();                         // the codes of t; those of t + 1 travel under its products
                 wait_lds();
-                th[S - 1] = 0;
-                if (t + S - 1 < count) th[S - 1] = load_group(t + S - 1);
+                uint32_t next = 0;
+                if (t + 1 < count) next = load_group(t + 1);
                 const int k0 = first_key + t * C::kStep;
-                attend(t, k0, th[0], th[0] == 0xffffffffu && k0 + 31 <= all_see);
-#pragma unroll
-                for (int x = 0; x + 1 < S; ++x) th[x] = th[x + 1];
+                attend(t, k0, there, there == 0xffffffffu && k0 + 31 <= all_see);
+                there = next;
             }
 #pragma unroll
             for (int x = 0; x < NQ; ++x) {
@@ -488,7 +474,7 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void paged_stream_kernel
                 for (int x = 0; x < NQ; ++x) store_rows(x, head, l[x], o[x]);
             }
         } else {
-            const Parts<64 * W, C::kRows, HG, DP, decltype(line)> parts(line, part, tickets, groups);
+            const Parts<kThreads, C::kRows, HG, DP, decltype(line)> parts(line, part, tickets, groups);
             if (active && kw == 0) {
                 float* const to = parts.sums(parts.me) + hw * C::kRows * DP;
 #pragma unroll
