@@ -4,8 +4,8 @@
 // a score exceeds it by 2^8; p rounded to bf16 for the second product, to two in rows of few keys; sums in
 // fp32).
 //
-// A workgroup of 4 waves owns 128 rows -- a row is a (token, query head) pair, the
-// heads of one KV head side by side, so that a causal tile's rows end within
+// A wave owns 32 rows, a workgroup 128 (4 waves), over the cache at heads of 128 256 (8 waves) -- a row is a
+// (token, query head) pair, the heads of one KV head side by side, so that a causal tile's rows end within
 // 128/G tokens -- and walks its keys in tiles of 64.  K and V tiles lie in LDS as
 // bf16 rows, two buffers of each; every wave reads them for its own 32 rows.
 //   S^T = K Q^T  on v_mfma_f32_32x32x16_bf16 (A: 32 keys x 16 channels, B: queries, held in
@@ -13,18 +13,19 @@
 //   O^T = V^T P^T: the probabilities of a lane are, as they are, its k-slots of the
 //     second operand when V^T is read with keys in the same order; the
 //     transposing LDS read (ds_read_b64_tr_b16: 4 keys of one channel per lane) does.
-// Two workgroups share a CU, so that one wave's exponentials run beside the
-// other's matrix instructions.
+// Two waves share a SIMD, so that one's exponentials run beside the other's matrix instructions: of two workgroups
+// (heads of 64, prompts of 128) or of one of eight waves (128 KB of LDS: the cache at heads of 128).  Heads of 256 take
+// all registers: one wave a SIMD.
 // Chunks of 16 bytes lie at slot c ^ f(key) of their row, so that the 16 lanes of
 // an LDS cycle (K: lanes l and l + 16, l % 16 < 8; V: 4 keys of 64 bytes) hit different banks.
 //
-// What bounds it: the matrix cores.  A prompt of 8191 tokens, 32 query and 8 KV heads of 128, takes 530 us,
-// 1.04 PFLOP/s (a large bf16 product of the card's library: 1.19); 9 prompts of 200..2100 tokens 155 us: each
-// 128 rows begin with an empty pipeline and end in a tile that is seen in part.  Over the cache the same
-// tile also turns 64 keys' codes into bf16 and scales scores and probabilities per key: 6 chunks of up to
-// 2000 rows over 100..6000 tokens take 765 us, 0.62 PFLOP/s; 256 rows a workgroup share that work (128: a
-// sixth more).  Not faster: the scores of the next tile under the sums of this one (spills), a raised wave
-// priority, output rows through LDS.
+// What bounds it: the matrix cores and the vector instructions beside them.  A prompt of 8191 tokens, 32 query and 8 KV
+// heads of 128, takes 520 to 548 us, 1.0 PFLOP/s (a large bf16 product of the card's library: 1.22), with the matrix
+// cores at work 49% of the time and the vector units 45%; 9 prompts of 200..2100 tokens 156 us: each 128 rows begin with
+// an empty pipeline and end in a tile that is seen in part.  Over the cache the same tile also turns 64 keys' codes into
+// bf16 and scales scores and probabilities per key: 6 chunks of up to 2000 rows over 100..6000 tokens take 720 us, 0.66
+// PFLOP/s (26% and 39%); 256 rows a workgroup share that work (128: a sixth more).  Not faster: the scores of the next
+// tile under the sums of this one (spills), a raised wave priority, output rows through LDS.
 #pragma once
 
 #include <type_traits>

@@ -108,6 +108,8 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     tree_attention_mask) N+1 each: the root's and the nodes'.  scale: 1/sqrt(D)
     if None.  Returns out bf16 [T, Hq, D]; given with cu_q, rows outside
     [cu_q[0], cu_q[B]) stay as they were (a new one holds anything there).
+    One kernel is chosen for all sequences, by their average rows: a call each for long
+    chunks and for single tokens is faster than one for both.
     workspace: paged_attention_workspace_bytes(T, B, Hq, H, D) bytes on the GPU, 16-byte
     aligned, zero-filled once and then kept for all calls of a stream.  Bring
     one: without it (or with one too small) every call makes a new one.

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import workloads as wl
-from oracle import attention as oa
+from oracle import attention as oa, e4m3
 from tests.attention_cases import paged_case, within
 from tests.attention_variants import reference
 from tests.gpu_util import dev_bf16, dev_f32, dev_i32, dev_u8, host_bf16_bits, need_gpu, say
@@ -101,3 +101,22 @@ def test_the_same_rows_by_the_stream_and_by_tiles(D, n, B, H):
     rel = lambda x, y: float(np.sqrt(np.sum((x - y) ** 2) / np.sum(y ** 2)))
     say(f"  error of tiles {rel(tiles[keep], out[keep]):.5f}, of the stream {rel(stream, out[keep]):.5f}, apart {rel(tiles[keep], stream):.5f}")
     assert not np.array_equal(tiles[keep], stream)       # (both kernels have run)
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("new,ctx,H,G,D", [([65, 65], 63, 32, 8, 128), ([40, 40], 63, 32, 4, 64), ([65, 65], 63, 16, 8, 256), ([65, 65], 20, 32, 8, 128)])
+def test_an_infinite_value_scale_in_tiles_of_few_keys(new, ctx, H, G, D, sign):
+    """Seen by every row of the first tiles (64 keys: all of a tile), whose weights enter as two bf16: inf - inf is NaN."""
+    p = need_gpu()
+    c = paged_case(73, new, [ctx] * 2, H, G, D)
+    slot = c["tables"][0, 0] * 16 + 3
+    c["vc"][slot, 1, 6] = 0x80
+    before = paged(p, c)
+    c["vs"][slot, 1] = sign * np.inf
+    out = paged(p, c)
+    hit = np.zeros(out.shape, bool)
+    hit[:new[0], G:2 * G] = True
+    np.testing.assert_array_equal(out[~hit], before[~hit])
+    code = e4m3.decode(c["vc"][slot, 1])
+    got = out[:new[0], G:2 * G]
+    np.testing.assert_array_equal(got, np.broadcast_to(np.where(code == 0, np.nan, np.copysign(np.inf, code * sign)), got.shape))
