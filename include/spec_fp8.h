@@ -507,7 +507,7 @@ spec_status spec_fp8_kv_cache_read(const uint8_t* k_cache, const uint8_t* v_cach
  * over the tokens seen (m_i: a reference within 2^8 of the largest s_ij); a row that sees none, or only scores
  * of -inf, is zeros.  What a row does not see has no influence on it, NaN codes and scales
  * included.  An infinite scale of a value seen gives infinities of its codes' signs, NaN where
- * the code is 0.  Products of q and codes are exact; they are summed, and the sums
+ * the code is 0 (either where p_ij is 0 or below fp32's range).  Products of q and codes are exact; they are summed, and the sums
  * of p and p*v accumulated, in fp32; p_ij * sv_j (or p_ij alone, where one
  * scale holds for the tensor) enters the second product in bf16: for few rows as the sum of
  * two (off by 2^-15 of its term at most), for many rounded once (2^-8), but for rows that

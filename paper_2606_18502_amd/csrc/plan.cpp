@@ -195,8 +195,9 @@ AcceptPlan plan_accept(int64_t B, int64_t k, int64_t V) {
 // 46/52, 256 66/88; at D = 256 of 192 rows 300/244, 256 306/302, 384 412/420, 1024 970/1061.  Few tiles: 8
 // sequences of 256 rows (64 tiles) 93/83, 4 of 512 (64) 98/94, 2 of 1024 (64) 104/104, one of 2048 (64) 140/159.
 // Those are sequences of equal rows; a batch that mixes a long chunk with single tokens takes one kernel for all of
-// them: 2048 rows over 4096 tokens beside 63 tokens 512 us, alone 250 and 59.  The choice also sets a weight's bits: 8 in tiles (rows of more than 64 keys), 15 in the stream.  The same rows
-// at the switch are off by 0.0023 of their size in tiles, by 0.0017 in the stream (the output's own rounding).
+// them: 2048 rows over 4096 tokens beside 63 tokens 512 us, alone 250 and 59.  The choice also sets a weight's bits: 8
+// in tiles (rows of more than 64 keys), 15 in the stream.  The same rows at the switch are off by 0.0023 of their size
+// in tiles, by 0.0017 in the stream (the output's own rounding).
 PagedPlan plan_paged(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t max_len) {
     PagedPlan p{0, 0, 1, false, 0, kAttnTicketBytes};
     if (D % 16 != 0) return p;
