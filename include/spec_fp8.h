@@ -68,6 +68,11 @@ typedef enum {
     SPEC_OUT_F32 = 1
 } spec_out_dtype;
 
+typedef enum {
+    SPEC_ROPE_HALVES = 0,      /* channels i and i + R/2 turn together                */
+    SPEC_ROPE_NEIGHBOURS = 1   /* channels 2i and 2i + 1 turn together                */
+} spec_rope_pairs;
+
 /*
  * spec_fp8_quantize -- rows of bf16 values to E4M3 codes with fp32 scales.
  *
@@ -119,6 +124,39 @@ spec_status spec_fp8_quantize(const void* x, int64_t rows, int64_t cols, int64_t
  */
 spec_status spec_silu_mul_bf16(const void* x, int64_t rows, int64_t cols, int64_t ld_x,
                                void* h, int64_t ld_h, void* stream);
+
+/*
+ * spec_fp8_rms_norm -- what stands before the QKV and the gate|up linear of a
+ * decoder layer (the Llama-family target, section 4): the residual's addition,
+ * the root-mean-square norm, and its quantization to E4M3 (section 3.2), in one
+ * pass over the rows.  For every row r:
+ *
+ *   h[c] = fl32(x[r,c] + residual[r,c])        (residual NULL: x[r,c])
+ *   sum[r,c] = bf16_RNE(h[c])                  the next residual   (sum NULL: not written)
+ *   y[c] = h[c] * w[c] / sqrt(mean_c h[c]^2 + eps)       in fp32, of h as it is before that rounding
+ *   y[r,c] = bf16_RNE(y[c])                                        (y NULL: not written)
+ *   PER_ROW:    s[r] = max(fl32(max_c |y[c]| / 448), 2^-100); scales[r] = s[r]   (written)
+ *   PER_TENSOR: s[r] = scales[0]                                                (read)
+ *   q[r,c] = E4M3(fl32(y[c] * fl32(1 / s[r])))                     (q NULL: no codes; scales is not looked at)
+ *
+ * with spec_fp8_quantize's E4M3(.); the codes are of y in fp32, not of its bf16 rounding.  At
+ * least one of q and y is given.  Sums are fp32, in an order that depends on cols alone.
+ * A row whose h holds an infinity or a NaN has NaN for all of y, codes 0x7F and scale 2^-100;
+ * finite rows stay finite also where their squares exceed fp32.  A weight that is not finite
+ * gives unspecified codes.
+ *
+ * x, residual  bf16 [rows, ld_x] / [rows, ld_residual]; weight bf16 [cols].
+ * sum, y  bf16 [rows, ld_sum] / [rows, ld_y]; each may be x or residual itself (same pointer and
+ *         stride; sum and y not the same), and overlaps no input otherwise.
+ * q       uint8 [rows, ld_q]; scales fp32 [rows] (PER_ROW) or [1] (PER_TENSOR; finite and > 0).
+ * Requirements: rows >= 0 (0 is a no-op), cols > 0, every stride in use >= cols (SPEC_ERR_SHAPE);
+ * cols % 8 == 0, cols <= 65536, rows < 2^31 (SPEC_ERR_UNSUPPORTED); 2^-60 <= eps < infinity
+ * (SPEC_ERR_VALUE); x, weight, one of q and y, and scales with q (SPEC_ERR_NULL); all of them 16-byte aligned, scales 4-byte,
+ * strides multiples of 8 (SPEC_ERR_ALIGN); mode PER_ROW or PER_TENSOR (SPEC_ERR_ENUM).
+ */
+spec_status spec_fp8_rms_norm(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, const void* weight,
+                              float eps, int64_t rows, int64_t cols, spec_scale_mode mode, float* scales, uint8_t* q,
+                              int64_t ld_q, void* sum, int64_t ld_sum, void* y, int64_t ld_y, void* stream);
 
 /*
  * spec_fp8_clip_count -- how many values a static per-tensor scale clips.
@@ -185,6 +223,44 @@ spec_status spec_fp8_kv_cache_write(const void* k, int64_t ld_k, const void* v, 
                                     uint8_t* k_cache, uint8_t* v_cache, void* stream);
 
 /*
+ * spec_fp8_rope_kv_cache_write -- the new tokens' queries and keys rotated by
+ * their positions, and the keys and values quantized into the paged FP8 KV
+ * cache: what stands between the QKV linear and the attention.  Pair i < R/2 of
+ * a head's first R channels, (x, y) = channels (i, i + R/2) (SPEC_ROPE_HALVES) or
+ * (2i, 2i + 1) (SPEC_ROPE_NEIGHBOURS), becomes
+ *
+ *   (x cos f - y sin f, y cos f + x sin f),   f = positions[t] * inv_freq[i]
+ *
+ * in fp32, with f in 64 bits and reduced to one turn there; channels from R on stay
+ * as they are.  Any scheme that stretches positions is a choice of inv_freq.
+ *
+ *   q_out[t] = bf16_RNE(rotated q[t])
+ *   k_out[t] = bf16_RNE(rotated k[t])       (k_out NULL: not written; spec_prompt_attention_bf16 takes it)
+ *   k_cache, k_scale, v_cache, v_scale at slot_mapping[t]: spec_fp8_kv_cache_write's encoding of the rotated
+ *            key rows in fp32 (not rounded to bf16 first) and of the value rows (bit for bit)
+ *
+ * A token whose slot is negative (padding) or >= num_slots is not stored; its q_out and k_out are
+ * written all the same.  Slots of different tokens must differ, as there.
+ *
+ * q        bf16 [T, ld_q], Hq heads of D (Hq = 0: keys and values alone; q and q_out are not looked at).
+ * k, v     bf16 [T, ld_k] / [T, ld_v], H heads of D; the column blocks of the QKV projection's output fit directly.
+ * q_out, k_out  bf16 [T, ld_q_out] / [T, ld_k_out]; may be q and k themselves (same pointer and stride), and
+ *          overlap no input otherwise.  Columns behind the heads keep their contents.
+ * positions int32 [T]; inv_freq fp64 [R/2], finite (of magnitude at most 1 or so: the angle is exact to 2^-52 of itself).
+ * slot_mapping, num_slots, mode, k_scale, v_scale, k_cache, v_cache: as spec_fp8_kv_cache_write.
+ * Requirements: those of spec_fp8_kv_cache_write; Hq >= 0, 0 < R <= D, ld_q and ld_q_out >= Hq*D, ld_k_out >= H*D
+ * (SPEC_ERR_SHAPE); R % 8 == 0, Hq and H <= 65535 (SPEC_ERR_UNSUPPORTED); q, q_out and k_out 16-byte aligned, their strides
+ * multiples of 8, positions 4-byte and inv_freq 8-byte aligned (SPEC_ERR_ALIGN); pairs one of the two (SPEC_ERR_ENUM).
+ * num_slots == 0 stores nothing: the caches and scales may be NULL.
+ */
+spec_status spec_fp8_rope_kv_cache_write(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v,
+                                         int64_t ld_v, const int32_t* positions, const double* inv_freq, int64_t R,
+                                         spec_rope_pairs pairs, const int64_t* slot_mapping, int64_t T, int64_t Hq,
+                                         int64_t H, int64_t D, int64_t num_slots, spec_scale_mode mode, float* k_scale,
+                                         float* v_scale, uint8_t* k_cache, uint8_t* v_cache, void* q_out,
+                                         int64_t ld_q_out, void* k_out, int64_t ld_k_out, void* stream);
+
+/*
  * spec_fp8_gemm -- the W8A8 linear layer (section 3.2):
  *
  *   acc[m,n] = sum_k dec(A[m,k]) * dec(W[n,k])     accumulated in fp32
@@ -248,6 +324,50 @@ spec_status spec_fp8_gemm(const uint8_t* a, int64_t lda, const float* a_scale, s
 spec_status spec_fp8_gemm_silu_mul(const uint8_t* a, int64_t lda, const float* a_scale, spec_scale_mode a_mode,
                                    const uint8_t* w, int64_t ldw, const float* w_scale, spec_scale_mode w_mode,
                                    int64_t M, int64_t I, int64_t K, void* h, int64_t ldh, void* stream);
+
+/*
+ * spec_fp4_quantize -- rows of bf16 weights to 4 bits: OCP MXFP4, that is E2M1
+ * codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) with one E8M0 scale
+ * 2^(byte - 127) for 32 of them.  A drafter that scores few rows is bound by reading its weights;
+ * these are half of E4M3's bytes.  For every row and group g of 32 columns:
+ *
+ *   e = clamp(floor(log2(r)) - 2, -100, 125), r the group's largest magnitude rounded (ties to even) to two
+ *       significant bits, so that it becomes 4 or 6 and saturates at 6 beyond the clamp alone
+ *   scales[r,g] = e + 127
+ *   code[r,c]   = E2M1_RNE_SAT(x[r,c] * 2^-e); the sign of zero is kept; column c in the low (c even) or high
+ *                 half of q[r, c/2]
+ *
+ * Non-finite inputs give unspecified codes.
+ *
+ * x bf16 [rows, ld_x]; q uint8 [rows, ld_q] (ld_q in bytes, >= cols/2); scales uint8 [rows, ld_scales], >= cols/32.
+ * Requirements: rows >= 0 (0 is a no-op), cols > 0 (SPEC_ERR_SHAPE); cols % 32 == 0, cols < 2^31 (SPEC_ERR_UNSUPPORTED);
+ * x and q 16-byte aligned, ld_x a multiple of 8 and ld_q of 16 (SPEC_ERR_ALIGN).
+ */
+spec_status spec_fp4_quantize(const void* x, int64_t rows, int64_t cols, int64_t ld_x, uint8_t* q, int64_t ld_q,
+                              uint8_t* scales, int64_t ld_scales, void* stream);
+
+/*
+ * spec_fp8_gemm_fp4 -- a linear layer with E4M3 activations and 4-bit weights
+ * (W4A8), for the few rows of a drafter's steps:
+ *
+ *   acc[m,n] = sum_g 2^(w_scale[n,g] - 127) sum_{k in g} dec(A[m,k]) * dec4(W[n,k])     accumulated in fp32
+ *   Y[m,n]   = fl32(acc[m,n] * sa(m))  then bf16 (RNE) or fp32
+ *
+ * A       uint8 E4M3 [M, lda] with a_scale fp32 [M] (PER_ROW) or [1] (PER_TENSOR), as spec_fp8_quantize and
+ *         spec_fp8_rms_norm leave them.  A NaN code makes its row of Y NaN.
+ * W       uint8 [N, ldw] packed codes (ldw in bytes) and w_scale uint8 [N, ld_w_scale], as spec_fp4_quantize leaves them,
+ *         or any MXFP4 weights of that layout; a scale byte of 255 is NaN and makes its column of Y NaN.
+ * Y       bf16 or fp32 [M, ldy], N <= ldy.
+ * Products are exact; the matrix cores' sums are those of spec_fp8_gemm.  The order of summation depends on N, K and M
+ * alone.  No workspace.
+ * Any M is computed, but weights are read once for every 64 rows: for many rows spec_fp8_gemm is made.
+ * Requirements: M >= 0 (0 is a no-op), N > 0, K > 0, lda >= K, ldw >= K/2, ld_w_scale >= K/32, ldy >= N (SPEC_ERR_SHAPE);
+ * K % 32 == 0, K < 2^31, N < 2^28, M <= 2^20 - 16 (SPEC_ERR_UNSUPPORTED); A, W and Y 16-byte aligned, lda and ldw
+ * multiples of 16, ldy of 8, a_scale 4-byte aligned (w_scale takes any stride and address) (SPEC_ERR_ALIGN).
+ */
+spec_status spec_fp8_gemm_fp4(const uint8_t* a, int64_t lda, const float* a_scale, spec_scale_mode a_mode,
+                              const uint8_t* w, int64_t ldw, const uint8_t* w_scale, int64_t ld_w_scale, int64_t M,
+                              int64_t N, int64_t K, void* y, int64_t ldy, spec_out_dtype out_dtype, void* stream);
 
 /*
  * spec_fp8_gemm_logit_stats -- the LM-head projection of the verify pass (the

@@ -39,6 +39,11 @@ from .ops import (  # noqa: F401
     calibrate,
     clip_count,
     silu_mul,
+    rms_norm,
+    rms_norm_quantize,
+    rope_kv_cache_write,
+    quantize_fp4,
+    gemm_fp4,
     kv_cache_write,
     kv_cache_read,
     paged_attention,

@@ -17,6 +17,7 @@ STATUS_NAMES = {0: "SPEC_OK", 1: "SPEC_ERR_NULL", 2: "SPEC_ERR_SHAPE", 3: "SPEC_
 SCALE_PER_ROW, SCALE_PER_TENSOR, SCALE_CALIBRATE = 0, 1, 2
 QIN_BF16, QIN_SILU_MUL_BF16 = 0, 1
 OUT_BF16, OUT_F32 = 0, 1
+ROPE_HALVES, ROPE_NEIGHBOURS = 0, 1
 
 EXPORTS = ("spec_fp8_quantize", "spec_silu_mul_bf16", "spec_fp8_kv_cache_write", "spec_fp8_clip_count", "spec_fp8_gemm_workspace_bytes", "spec_fp8_gemm",
            "spec_fp8_gemm_silu_mul", "spec_logit_stats_count", "spec_fp8_gemm_logit_stats",
@@ -24,7 +25,8 @@ EXPORTS = ("spec_fp8_quantize", "spec_silu_mul_bf16", "spec_fp8_kv_cache_write",
            "spec_verify_accept_stats",
            "spec_verify_accept_tree_workspace_bytes", "spec_verify_accept_tree", "spec_tree_attention_mask",
            "spec_fp8_kv_cache_read", "spec_fp8_paged_attention_workspace_bytes", "spec_fp8_paged_attention",
-           "spec_prompt_attention_bf16",
+           "spec_prompt_attention_bf16", "spec_fp8_rms_norm", "spec_fp8_rope_kv_cache_write", "spec_fp4_quantize",
+           "spec_fp8_gemm_fp4",
            "spec_status_string", "spec_last_hip_error", "spec_version")
 
 _lib = None
@@ -62,6 +64,15 @@ def declare(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.spec_fp8_clip_count.restype = i32
     lib.spec_fp8_kv_cache_write.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, i64, i32, vp, vp, vp, vp, vp]
     lib.spec_fp8_kv_cache_write.restype = i32
+    lib.spec_fp8_rms_norm.argtypes = [vp, i64, vp, i64, vp, f32, i64, i64, i32, vp, vp, i64, vp, i64, vp, i64, vp]
+    lib.spec_fp8_rms_norm.restype = i32
+    lib.spec_fp8_rope_kv_cache_write.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, i64, i32, vp, i64, i64, i64, i64, i64,
+                                                 i32, vp, vp, vp, vp, vp, i64, vp, i64, vp]
+    lib.spec_fp8_rope_kv_cache_write.restype = i32
+    lib.spec_fp4_quantize.argtypes = [vp, i64, i64, i64, vp, i64, vp, i64, vp]
+    lib.spec_fp4_quantize.restype = i32
+    lib.spec_fp8_gemm_fp4.argtypes = [vp, i64, vp, i32, vp, i64, vp, i64, i64, i64, i64, vp, i64, i32, vp]
+    lib.spec_fp8_gemm_fp4.restype = i32
     lib.spec_fp8_kv_cache_read.argtypes = [vp, vp, vp, vp, i32, vp, i64, i64, i64, i64, vp, i64, vp, i64, vp]
     lib.spec_fp8_kv_cache_read.restype = i32
     lib.spec_fp8_paged_attention_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]

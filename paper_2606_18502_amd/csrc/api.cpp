@@ -67,6 +67,107 @@ spec_status spec_fp8_kv_cache_write(const void* k, int64_t ld_k, const void* v, 
         as_stream(stream)));
 }
 
+spec_status spec_fp8_rms_norm(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, const void* weight,
+                              float eps, int64_t rows, int64_t cols, spec_scale_mode mode, float* scales, uint8_t* q,
+                              int64_t ld_q, void* sum, int64_t ld_sum, void* y, int64_t ld_y, void* stream) {
+    const spec_status st = specfp8::check_rms_norm(x, ld_x, residual, ld_residual, weight, eps, rows, cols, (int)mode,
+                                                   scales, q, ld_q, sum, ld_sum, y, ld_y);
+    if (st != SPEC_OK || rows == 0) return st;
+    if (!specfp8::launch_rms_norm) return from_hip(hipErrorNotSupported);
+    specfp8::NormArgs a;
+    a.x = reinterpret_cast<const uint16_t*>(x);
+    a.residual = reinterpret_cast<const uint16_t*>(residual);
+    a.weight = reinterpret_cast<const uint16_t*>(weight);
+    a.sum = reinterpret_cast<uint16_t*>(sum);
+    a.y = reinterpret_cast<uint16_t*>(y);
+    a.q = q;
+    a.scales = scales;
+    a.ld_x = ld_x;
+    a.ld_r = ld_residual;
+    a.ld_sum = ld_sum;
+    a.ld_y = ld_y;
+    a.ld_q = ld_q;
+    a.rows = rows;
+    a.cols = (int32_t)cols;
+    a.per_tensor = mode == SPEC_SCALE_PER_TENSOR ? 1 : 0;
+    a.eps = eps;
+    return from_hip(specfp8::launch_rms_norm(a, as_stream(stream)));
+}
+
+spec_status spec_fp8_rope_kv_cache_write(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v,
+                                         int64_t ld_v, const int32_t* positions, const double* inv_freq, int64_t R,
+                                         spec_rope_pairs pairs, const int64_t* slot_mapping, int64_t T, int64_t Hq,
+                                         int64_t H, int64_t D, int64_t num_slots, spec_scale_mode mode, float* k_scale,
+                                         float* v_scale, uint8_t* k_cache, uint8_t* v_cache, void* q_out,
+                                         int64_t ld_q_out, void* k_out, int64_t ld_k_out, void* stream) {
+    const spec_status st = specfp8::check_rope_kv_cache_write(
+        q, ld_q, k, ld_k, v, ld_v, positions, inv_freq, R, (int)pairs, slot_mapping, T, Hq, H, D, num_slots, (int)mode,
+        k_scale, v_scale, k_cache, v_cache, q_out, ld_q_out, k_out, ld_k_out);
+    if (st != SPEC_OK || T == 0) return st;
+    if (!specfp8::launch_rope_kv_write) return from_hip(hipErrorNotSupported);
+    specfp8::RopeArgs a;
+    a.q = reinterpret_cast<const uint16_t*>(q);
+    a.k = reinterpret_cast<const uint16_t*>(k);
+    a.v = reinterpret_cast<const uint16_t*>(v);
+    a.q_out = reinterpret_cast<uint16_t*>(q_out);
+    a.k_out = reinterpret_cast<uint16_t*>(k_out);
+    a.positions = positions;
+    a.inv_freq = inv_freq;
+    a.slot = slot_mapping;
+    a.k_scale = k_scale;
+    a.v_scale = v_scale;
+    a.k_cache = k_cache;
+    a.v_cache = v_cache;
+    a.ld_q = ld_q;
+    a.ld_k = ld_k;
+    a.ld_v = ld_v;
+    a.ld_q_out = ld_q_out;
+    a.ld_k_out = ld_k_out;
+    a.T = T;
+    a.num_slots = num_slots;
+    a.Hq = (int32_t)Hq;
+    a.H = (int32_t)H;
+    a.D = (int32_t)D;
+    a.R = (int32_t)R;
+    a.per_tensor = mode == SPEC_SCALE_PER_TENSOR ? 1 : 0;
+    a.log_parts = 0;
+    return from_hip(specfp8::launch_rope_kv_write(a, pairs == SPEC_ROPE_NEIGHBOURS, as_stream(stream)));
+}
+
+spec_status spec_fp4_quantize(const void* x, int64_t rows, int64_t cols, int64_t ld_x, uint8_t* q, int64_t ld_q,
+                              uint8_t* scales, int64_t ld_scales, void* stream) {
+    const spec_status st = specfp8::check_fp4_quantize(x, rows, cols, ld_x, q, ld_q, scales, ld_scales);
+    if (st != SPEC_OK || rows == 0) return st;
+    if (!specfp8::launch_fp4_quantize) return from_hip(hipErrorNotSupported);
+    return from_hip(specfp8::launch_fp4_quantize(reinterpret_cast<const uint16_t*>(x), rows, cols, ld_x, q, ld_q, scales,
+                                                 ld_scales, as_stream(stream)));
+}
+
+spec_status spec_fp8_gemm_fp4(const uint8_t* a, int64_t lda, const float* a_scale, spec_scale_mode a_mode,
+                              const uint8_t* w, int64_t ldw, const uint8_t* w_scale, int64_t ld_w_scale, int64_t M,
+                              int64_t N, int64_t K, void* y, int64_t ldy, spec_out_dtype out_dtype, void* stream) {
+    const spec_status st = specfp8::check_gemm_fp4(a, lda, a_scale, (int)a_mode, w, ldw, w_scale, ld_w_scale, M, N, K, y,
+                                                   ldy, (int)out_dtype);
+    if (st != SPEC_OK || M == 0) return st;
+    if (!specfp8::launch_gemm_fp4) return from_hip(hipErrorNotSupported);
+    specfp8::Fp4Args g;
+    g.a = a;
+    g.w = w;
+    g.w_scale = w_scale;
+    g.a_scale = a_scale;
+    g.y = y;
+    g.lda = lda;
+    g.ldw = ldw;
+    g.ld_ws = ld_w_scale;
+    g.ldy = ldy;
+    g.M = M;
+    g.N = N;
+    g.K = K;
+    g.per_tensor = a_mode == SPEC_SCALE_PER_TENSOR ? 1 : 0;
+    g.out_f32 = out_dtype == SPEC_OUT_F32 ? 1 : 0;
+    return from_hip(specfp8::launch_gemm_fp4(g, as_stream(stream)));
+}
+
 spec_status spec_fp8_kv_cache_read(const uint8_t* k_cache, const uint8_t* v_cache, const float* k_scale,
                                    const float* v_scale, spec_scale_mode mode, const int64_t* slot_mapping, int64_t T,
                                    int64_t H, int64_t D, int64_t num_slots, void* k, int64_t ld_k, void* v,

@@ -1,5 +1,6 @@
 // The FP8 GEMM (gemm_kernel.hpp): the choice of the kernel for a plan, and the
 // path for operands whose rows lie too far apart for it.
+#include "fp4.hpp"
 #include "gemm_kernel.hpp"
 
 namespace specfp8 {

@@ -36,6 +36,47 @@ SPEC_DEVICE_SIDE hipError_t launch_kv_cache_read(const uint8_t* k_cache, const u
                                                  int64_t T, int64_t H, int64_t D, int64_t num_slots, uint16_t* k,
                                                  int64_t ld_k, uint16_t* v, int64_t ld_v, hipStream_t stream);
 
+// ---- norm.hpp, in quantize.hip
+// Root-mean-square norm of rows ([rows][ld] bf16), the residual added first (or NULL); its sum, values and codes
+// (each or NULL) as include/spec_fp8.h states them.
+struct NormArgs {
+    const uint16_t *x, *residual, *weight;
+    uint16_t *sum, *y;
+    uint8_t* q;
+    float* scales;
+    int64_t ld_x, ld_r, ld_sum, ld_y, ld_q, rows;
+    int32_t cols, per_tensor;
+    float eps;
+};
+SPEC_DEVICE_SIDE hipError_t launch_rms_norm(const NormArgs& a, hipStream_t stream);
+
+// ---- rope.hpp, in kvcache.hip
+// Queries and keys rotated by their positions; keys and values to the paged cache (include/spec_fp8.h).
+struct RopeArgs {
+    const uint16_t *q, *k, *v;
+    uint16_t *q_out, *k_out;                 // bf16; k_out may be NULL
+    const int32_t* positions;
+    const double* inv_freq;
+    const int64_t* slot;
+    float *k_scale, *v_scale;
+    uint8_t *k_cache, *v_cache;
+    int64_t ld_q, ld_k, ld_v, ld_q_out, ld_k_out, T, num_slots;
+    int32_t Hq, H, D, R, per_tensor, log_parts;
+};
+SPEC_DEVICE_SIDE hipError_t launch_rope_kv_write(const RopeArgs& a, bool interleaved, hipStream_t stream);
+
+// ---- fp4.hpp, in gemm.hip
+SPEC_DEVICE_SIDE hipError_t launch_fp4_quantize(const uint16_t* x, int64_t rows, int64_t cols, int64_t ld_x, uint8_t* q,
+                                                int64_t ld_q, uint8_t* scales, int64_t ld_s, hipStream_t stream);
+struct Fp4Args {
+    const uint8_t *a, *w, *w_scale;          // codes [M][lda]; packed codes [N][ldw], scales [N][ld_ws] (bytes)
+    const float* a_scale;
+    void* y;
+    int64_t lda, ldw, ld_ws, ldy, M, N, K;
+    int32_t per_tensor, out_f32;
+};
+SPEC_DEVICE_SIDE hipError_t launch_gemm_fp4(const Fp4Args& a, hipStream_t stream);
+
 // ---- gemm.hip
 struct GemmPlan {
     int kind;              // tile configuration (plan.hpp, kTiles)

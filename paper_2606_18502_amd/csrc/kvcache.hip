@@ -15,6 +15,7 @@
 
 #include "device_common.hpp"
 #include "kernels.hpp"
+#include "rope.hpp"
 
 namespace specfp8 {
 

@@ -7,6 +7,8 @@
 
 namespace specfp8 {
 
+constexpr int64_t kNormMaxCols = 65536;      // of a norm's row: its sums stay in registers
+
 // ---- FP8 GEMM tiles ---------------------------------------------------------
 // A tile is a WM x WN grid of waves, each wave holding WTM x WTN blocks of
 // 16x16 outputs; STAGES LDS buffers rotate through the K-loop.  lspan8: a

@@ -14,6 +14,7 @@
 // 65536 elements take a second pass that re-reads the row.
 #include "device_common.hpp"
 #include "kernels.hpp"
+#include "norm.hpp"
 
 namespace specfp8 {
 

@@ -587,6 +587,216 @@ SPEC_PY(py_gemm) {
     END_HANDLE_TH_ERRORS
 }
 
+// A 2-D tensor of these sizes beside `like`; returns its row stride.
+int64_t like_rows(const Tensor& t, int64_t rows, int64_t cols, const Tensor& like, const char* name) {
+    const int64_t ld = rowmajor(t, name);
+    if (t.size(0) != rows || t.size(1) != cols)
+        value_error("%s must be [%lld, %lld]", name, (long long)rows, (long long)cols);
+    same_device(t, like, name);
+    return ld;
+}
+
+// rms_norm(x, weight, eps, residual, residual_out, out): (y, sum or None)
+// rms_norm_quantize(x, weight, eps, residual, per_tensor_scale, residual_out, normed, out, scales): (codes, scales, sum or None)
+struct NormCall {
+    const Tensor &x, &w;
+    int64_t rows, cols, ld, ld_r = 0, ld_sum = 0;
+    const void* residual = nullptr;
+    Out sum;
+    NormCall(PyObject* px, PyObject* pw, PyObject* pr, PyObject* psum)
+        : x(dev(px, ScalarType::BFloat16, "x")), w(dev(pw, ScalarType::BFloat16, "weight")), rows(0), cols(0),
+          ld(rowmajor(x, "x")) {
+        rows = x.size(0);
+        cols = x.size(1);
+        need(w.dim() == 1 && w.size(0) == cols && w.is_contiguous(), "weight must be a contiguous bf16 [cols]");
+        same_device(w, x, "weight");
+        if (pr != Py_None) {
+            const Tensor& r = dev(pr, ScalarType::BFloat16, "residual");
+            ld_r = like_rows(r, rows, cols, x, "residual");
+            residual = r.data_ptr();
+        }
+        if (pr != Py_None || psum != Py_None) {
+            sum = out_arg(psum, ScalarType::BFloat16, "residual_out",
+                          [&] { return new_empty({rows, cols}, ScalarType::BFloat16, x); });
+            ld_sum = like_rows(sum.t, rows, cols, x, "residual_out");
+        }
+    }
+    void* sum_ptr() const { return sum.t.defined() ? sum.t.data_ptr() : nullptr; }
+    PyObject* release_sum() {
+        if (sum.t.defined()) return sum.release();
+        Py_RETURN_NONE;
+    }
+};
+
+SPEC_PY(py_rms_norm) {
+    HANDLE_TH_ERRORS
+    args(n, 6);
+    NormCall c(a[0], a[1], a[3], a[4]);
+    const float eps = number(a[2]);
+    const OnDevice on(c.x);
+    Out out = out_arg(a[5], ScalarType::BFloat16, "out",
+                      [&] { return new_empty({c.rows, c.cols}, ScalarType::BFloat16, c.x); });
+    const int64_t ld_y = like_rows(out.t, c.rows, c.cols, c.x, "out");
+    need(!c.sum_ptr() || c.rows == 0 || out.t.data_ptr() != c.sum_ptr(), "out and residual_out must differ");
+    void* const s = stream();
+    check("spec_fp8_rms_norm", call([&] {
+              return spec_fp8_rms_norm(c.x.data_ptr(), c.ld, c.residual, c.ld_r, c.w.data_ptr(), eps, c.rows, c.cols,
+                                       SPEC_SCALE_PER_ROW, nullptr, nullptr, 0, c.sum_ptr(), c.ld_sum, out.t.data_ptr(),
+                                       ld_y, s);
+          }));
+    PyObject* const sum = c.release_sum();
+    PyObject* const y = out.release();
+    return Py_BuildValue("(NN)", y, sum);
+    END_HANDLE_TH_ERRORS
+}
+
+SPEC_PY(py_rms_norm_quantize) {
+    HANDLE_TH_ERRORS
+    args(n, 9);
+    NormCall c(a[0], a[1], a[3], a[5]);
+    const float eps = number(a[2]);
+    const OnDevice on(c.x);
+    Out out = out_arg(a[7], ScalarType::Byte, "out", [&] { return new_empty({c.rows, c.cols}, ScalarType::Byte, c.x); });
+    const int64_t ld_q = like_rows(out.t, c.rows, c.cols, c.x, "out");
+    const bool fixed = a[4] != Py_None;
+    Out sc = fixed ? out_arg(a[4], ScalarType::Float, "per_tensor_scale", [] { return Tensor(); })
+                   : out_arg(a[8], ScalarType::Float, "scales",
+                             [&] { return new_empty({c.rows}, ScalarType::Float, c.x); });
+    need(sc.t.is_contiguous() && sc.t.numel() == (fixed ? 1 : c.rows),
+         fixed ? "per_tensor_scale must hold one fp32 value" : "scales must be a contiguous fp32 [rows]");
+    same_device(sc.t, c.x, "scales");
+    void* y = nullptr;
+    int64_t ld_y = 0;
+    if (a[6] != Py_None) {
+        const Tensor& t = dev(a[6], ScalarType::BFloat16, "normed");
+        ld_y = like_rows(t, c.rows, c.cols, c.x, "normed");
+        y = t.data_ptr();
+        need(!c.sum_ptr() || c.rows == 0 || y != c.sum_ptr(), "normed and residual_out must differ");
+    }
+    void* const s = stream();
+    check("spec_fp8_rms_norm", call([&] {
+              return spec_fp8_rms_norm(c.x.data_ptr(), c.ld, c.residual, c.ld_r, c.w.data_ptr(), eps, c.rows, c.cols,
+                                       fixed ? SPEC_SCALE_PER_TENSOR : SPEC_SCALE_PER_ROW, (float*)sc.t.data_ptr(),
+                                       (uint8_t*)out.t.data_ptr(), ld_q, c.sum_ptr(), c.ld_sum, y, ld_y, s);
+          }));
+    PyObject* const sum = c.release_sum();
+    PyObject* const q = out.release();
+    PyObject* const scales = sc.release();
+    return Py_BuildValue("(NNN)", q, scales, sum);
+    END_HANDLE_TH_ERRORS
+}
+
+// rope_kv_cache_write(q, k, v, positions, inv_freq, slot_mapping, k_cache, v_cache, k_scale, v_scale, per_tensor,
+//                     interleaved, q_out, k_out): q_out
+SPEC_PY(py_rope_kv_cache_write) {
+    HANDLE_TH_ERRORS
+    args(n, 14);
+    const Tensor& q = dev(a[0], ScalarType::BFloat16, "q");
+    const Tensor& k = dev(a[1], ScalarType::BFloat16, "k");
+    const Tensor& v = dev(a[2], ScalarType::BFloat16, "v");
+    const Heads hq = heads(q, "q"), hk = heads(k, "k"), hv = heads(v, "v");
+    const int64_t T = hk.T;
+    need(hq.T == T && hq.D == hk.D && v.sizes() == k.sizes(), "q, k and v must be [T, heads, D] with one T and D");
+    same_device(q, k, "q");
+    same_device(v, k, "v");
+    const Cache c = cache(a[6], a[7], a[8], a[9], truth(a[10]));
+    need(c.H == hk.H && c.D == hk.D, "k and the caches must have the same heads");
+    same_device(c.k, k, "k_cache");
+    const int32_t* const pos = int_vector(a[3], T, k, "positions", "positions must be a contiguous int32 [T]");
+    const Tensor& freq = dev(a[4], ScalarType::Double, "inv_freq");
+    need(freq.dim() == 1 && freq.is_contiguous(), "inv_freq must be a contiguous fp64 [R / 2]");
+    same_device(freq, k, "inv_freq");
+    const Tensor& slots = dev(a[5], ScalarType::Long, "slot_mapping");
+    need(slots.dim() == 1 && slots.size(0) == T && slots.is_contiguous(), "slot_mapping must be a contiguous int64 [T]");
+    same_device(slots, k, "slot_mapping");
+    const OnDevice on(k);
+    Out q_out = out_arg(a[12], ScalarType::BFloat16, "q_out",
+                        [&] { return new_empty({T, hq.H, hq.D}, ScalarType::BFloat16, k); });
+    const Heads ho = heads(q_out.t, "q_out");
+    need(ho.T == T && ho.H == hq.H && ho.D == hq.D, "q_out must be [T, Hq, D] like q");
+    same_device(q_out.t, k, "q_out");
+    void* k_out = nullptr;
+    int64_t ld_ko = 0;
+    if (a[13] != Py_None) {
+        const Tensor& t = dev(a[13], ScalarType::BFloat16, "k_out");
+        const Heads h = heads(t, "k_out");
+        need(h.T == T && h.H == hk.H && h.D == hk.D, "k_out must be [T, H, D] like k");
+        same_device(t, k, "k_out");
+        k_out = t.data_ptr();
+        ld_ko = h.ld;
+    }
+    const spec_rope_pairs pairs = truth(a[11]) ? SPEC_ROPE_NEIGHBOURS : SPEC_ROPE_HALVES;
+    void* const s = stream();
+    check("spec_fp8_rope_kv_cache_write", call([&] {
+              return spec_fp8_rope_kv_cache_write(
+                  q.data_ptr(), hq.ld, k.data_ptr(), hk.ld, v.data_ptr(), hv.ld, pos, (const double*)freq.data_ptr(),
+                  2 * freq.size(0), pairs, (const int64_t*)slots.data_ptr(), T, hq.H, hk.H, hk.D, c.slots, c.mode,
+                  (float*)c.ks.data_ptr(), (float*)c.vs.data_ptr(), (uint8_t*)c.k.data_ptr(), (uint8_t*)c.v.data_ptr(),
+                  q_out.t.data_ptr(), ho.ld, k_out, ld_ko, s);
+          }));
+    return q_out.release();
+    END_HANDLE_TH_ERRORS
+}
+
+// quantize_fp4(x, out, scales)
+SPEC_PY(py_quantize_fp4) {
+    HANDLE_TH_ERRORS
+    args(n, 3);
+    const Tensor& x = dev(a[0], ScalarType::BFloat16, "x");
+    const int64_t ld = rowmajor(x, "x"), rows = x.size(0), cols = x.size(1);
+    const OnDevice on(x);
+    Out q = out_arg(a[1], ScalarType::Byte, "out", [&] { return new_empty({rows, cols / 2}, ScalarType::Byte, x); });
+    Out e = out_arg(a[2], ScalarType::Byte, "scales", [&] { return new_empty({rows, cols / 32}, ScalarType::Byte, x); });
+    const int64_t ld_q = like_rows(q.t, rows, cols / 2, x, "out"), ld_e = like_rows(e.t, rows, cols / 32, x, "scales");
+    void* const s = stream();
+    check("spec_fp4_quantize", call([&] {
+              return spec_fp4_quantize(x.data_ptr(), rows, cols, ld, (uint8_t*)q.t.data_ptr(), ld_q,
+                                       (uint8_t*)e.t.data_ptr(), ld_e, s);
+          }));
+    return pair(q, e);
+    END_HANDLE_TH_ERRORS
+}
+
+// gemm_fp4(a, sa, w, sw, out_dtype_is_f32 (None: not a dtype the kernel writes), out)
+SPEC_PY(py_gemm_fp4) {
+    HANDLE_TH_ERRORS
+    args(n, 6);
+    const Tensor& x = dev(a[0], ScalarType::Byte, "a");
+    const Tensor& sa = dev(a[1], ScalarType::Float, "sa");
+    const Tensor& w = dev(a[2], ScalarType::Byte, "w");
+    const Tensor& sw = dev(a[3], ScalarType::Byte, "sw");
+    const int64_t lda = rowmajor(x, "a"), ldw = rowmajor(w, "w"), ld_sw = rowmajor(sw, "sw");
+    const int64_t M = x.size(0), K = x.size(1), N = w.size(0);
+    need(w.size(1) * 2 == K, "w must be [N, K/2], two codes a byte, with the activations' K");
+    need(sw.size(0) == N && sw.size(1) == K / 32, "sw must be [N, K/32]");
+    const bool fixed = sa.numel() == 1 && M != 1;
+    need(sa.is_contiguous() && (fixed || sa.numel() >= M), "sa must hold M per-row scales or one per-tensor scale");
+    same_device(sa, x, "sa");
+    same_device(w, x, "w");
+    same_device(sw, x, "sw");
+    const OnDevice on(x);
+    Out out;
+    if (a[5] == Py_None) {
+        need(a[4] != Py_None, "out must be bf16 or fp32");
+        out.t = padded_rows(M, N, truth(a[4]) ? ScalarType::Float : ScalarType::BFloat16, x);
+    } else {
+        out.t = dev_any(a[5], "out");
+        out.given = a[5];
+        need(out.t.scalar_type() == ScalarType::BFloat16 || out.t.scalar_type() == ScalarType::Float,
+             "out must be bf16 or fp32");
+    }
+    const spec_out_dtype odt = out.t.scalar_type() == ScalarType::Float ? SPEC_OUT_F32 : SPEC_OUT_BF16;
+    const int64_t ldy = like_rows(out.t, M, N, x, "out");
+    void* const s = stream();
+    check("spec_fp8_gemm_fp4", call([&] {
+              return spec_fp8_gemm_fp4((const uint8_t*)x.data_ptr(), lda, (const float*)sa.data_ptr(),
+                                       fixed ? SPEC_SCALE_PER_TENSOR : SPEC_SCALE_PER_ROW, (const uint8_t*)w.data_ptr(),
+                                       ldw, (const uint8_t*)sw.data_ptr(), ld_sw, M, N, K, out.t.data_ptr(), ldy, odt, s);
+          }));
+    return out.release();
+    END_HANDLE_TH_ERRORS
+}
+
 // gemm_silu_mul(a, sa, w, sw, out)
 SPEC_PY(py_gemm_silu_mul) {
     HANDLE_TH_ERRORS
@@ -811,6 +1021,11 @@ PyMethodDef g_methods[] = {
     SPEC_METHOD(kv_cache_read),
     SPEC_METHOD(paged_attention),
     SPEC_METHOD(prompt_attention),
+    SPEC_METHOD(rms_norm),
+    SPEC_METHOD(rms_norm_quantize),
+    SPEC_METHOD(rope_kv_cache_write),
+    SPEC_METHOD(quantize_fp4),
+    SPEC_METHOD(gemm_fp4),
     SPEC_METHOD(gemm),
     SPEC_METHOD(gemm_silu_mul),
     SPEC_METHOD(gemm_logit_stats),

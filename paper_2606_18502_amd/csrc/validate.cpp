@@ -70,6 +70,82 @@ spec_status check_kv_cache_write(const void* k, int64_t ld_k, const void* v, int
     return SPEC_OK;
 }
 
+spec_status check_rms_norm(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, const void* weight,
+                           float eps, int64_t rows, int64_t cols, int mode, const float* scales, const void* q,
+                           int64_t ld_q, const void* sum, int64_t ld_sum, const void* y, int64_t ld_y) {
+    if (mode != SPEC_SCALE_PER_ROW && mode != SPEC_SCALE_PER_TENSOR) return SPEC_ERR_ENUM;
+    if (rows < 0 || cols <= 0) return SPEC_ERR_SHAPE;
+    if (ld_x < cols || (residual && ld_residual < cols) || (q && ld_q < cols) || (sum && ld_sum < cols) ||
+        (y && ld_y < cols))
+        return SPEC_ERR_SHAPE;
+    if (cols % 8 != 0 || cols > kNormMaxCols || rows > kMaxGrid) return SPEC_ERR_UNSUPPORTED;
+    if (!(eps >= 0x1p-60f) || !isfinite(eps)) return SPEC_ERR_VALUE;
+    if (rows == 0) return SPEC_OK;
+    if (!x || !weight || (!q && !y) || (q && !scales)) return SPEC_ERR_NULL;
+    if (!aligned16(x) || !aligned16(weight) || !aligned16(residual) || !aligned16(q) || !aligned16(sum) || !aligned16(y))
+        return SPEC_ERR_ALIGN;
+    if (ld_x % 8 != 0 || (residual && ld_residual % 8 != 0) || (q && ld_q % 8 != 0) || (sum && ld_sum % 8 != 0) ||
+        (y && ld_y % 8 != 0))
+        return SPEC_ERR_ALIGN;
+    if (q && (reinterpret_cast<uintptr_t>(scales) & 3u) != 0) return SPEC_ERR_ALIGN;
+    return SPEC_OK;
+}
+
+spec_status check_rope_kv_cache_write(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v,
+                                      int64_t ld_v, const int32_t* positions, const double* inv_freq, int64_t R,
+                                      int pairs, const int64_t* slot_mapping, int64_t T, int64_t Hq, int64_t H,
+                                      int64_t D, int64_t num_slots, int mode, const float* k_scale,
+                                      const float* v_scale, const void* k_cache, const void* v_cache,
+                                      const void* q_out, int64_t ld_q_out, const void* k_out, int64_t ld_k_out) {
+    if (pairs != SPEC_ROPE_HALVES && pairs != SPEC_ROPE_NEIGHBOURS) return SPEC_ERR_ENUM;
+    if (Hq < 0 || R <= 0 || R > D) return SPEC_ERR_SHAPE;
+    if (R % 8 != 0) return SPEC_ERR_UNSUPPORTED;
+    // the cache write's rules; an empty cache stores nothing
+    const bool empty = num_slots == 0;
+    static const float unused = 0.0f;
+    const spec_status st = check_kv_cache_write(k, ld_k, v, ld_v, slot_mapping, T, H, D, num_slots, mode,
+                                                empty && !k_scale ? &unused : k_scale,
+                                                empty && !v_scale ? &unused : v_scale, empty ? k : k_cache,
+                                                empty ? v : v_cache);
+    if (st == SPEC_ERR_ENUM || st == SPEC_ERR_SHAPE) return st;
+    if (Hq > kMaxGridY || H > kMaxGridY) return SPEC_ERR_UNSUPPORTED;
+    if (ld_q < Hq * D || (Hq > 0 && ld_q_out < Hq * D) || (k_out && ld_k_out < H * D)) return SPEC_ERR_SHAPE;
+    if (st != SPEC_OK || T == 0) return st;
+    if (!positions || !inv_freq || (Hq > 0 && (!q || !q_out))) return SPEC_ERR_NULL;
+    if (Hq > 0 && (ld_q % 8 != 0 || ld_q_out % 8 != 0 || !aligned16(q) || !aligned16(q_out))) return SPEC_ERR_ALIGN;
+    if (k_out && (ld_k_out % 8 != 0 || !aligned16(k_out))) return SPEC_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(positions) & 3u) != 0 || (reinterpret_cast<uintptr_t>(inv_freq) & 7u) != 0)
+        return SPEC_ERR_ALIGN;
+    return SPEC_OK;
+}
+
+spec_status check_fp4_quantize(const void* x, int64_t rows, int64_t cols, int64_t ld_x, const void* q, int64_t ld_q,
+                               const void* scales, int64_t ld_scales) {
+    if (rows < 0 || cols <= 0) return SPEC_ERR_SHAPE;
+    if (ld_x < cols || ld_q < cols / 2 || ld_scales < cols / 32) return SPEC_ERR_SHAPE;
+    if (cols % 32 != 0 || cols > kMaxGrid) return SPEC_ERR_UNSUPPORTED;
+    if (rows == 0) return SPEC_OK;
+    if (!x || !q || !scales) return SPEC_ERR_NULL;
+    if (ld_x % 8 != 0 || ld_q % 16 != 0 || !aligned16(x) || !aligned16(q)) return SPEC_ERR_ALIGN;
+    return SPEC_OK;
+}
+
+spec_status check_gemm_fp4(const void* a, int64_t lda, const float* a_scale, int a_mode, const void* w, int64_t ldw,
+                           const void* w_scale, int64_t ld_w_scale, int64_t M, int64_t N, int64_t K, const void* y,
+                           int64_t ldy, int out_dtype) {
+    if (a_mode != SPEC_SCALE_PER_ROW && a_mode != SPEC_SCALE_PER_TENSOR) return SPEC_ERR_ENUM;
+    if (out_dtype != SPEC_OUT_BF16 && out_dtype != SPEC_OUT_F32) return SPEC_ERR_ENUM;
+    if (M < 0 || N <= 0 || K <= 0) return SPEC_ERR_SHAPE;
+    if (lda < K || ldw < K / 2 || ld_w_scale < K / 32 || ldy < N) return SPEC_ERR_SHAPE;
+    if (K % 32 != 0 || K > kMaxGrid || N >= 1LL << 28 || M > 16 * kMaxGridY) return SPEC_ERR_UNSUPPORTED;
+    if (M == 0) return SPEC_OK;
+    if (!a || !a_scale || !w || !w_scale || !y) return SPEC_ERR_NULL;
+    if (lda % 16 != 0 || ldw % 16 != 0 || ldy % 8 != 0 || !aligned16(a) || !aligned16(w) || !aligned16(y))
+        return SPEC_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(a_scale) & 3u) != 0) return SPEC_ERR_ALIGN;
+    return SPEC_OK;
+}
+
 spec_status check_kv_cache_read(const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
                                 int mode, const int64_t* slot_mapping, int64_t T, int64_t H, int64_t D,
                                 int64_t num_slots, const void* k, int64_t ld_k, const void* v, int64_t ld_v) {

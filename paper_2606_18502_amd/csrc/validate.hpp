@@ -23,6 +23,20 @@ spec_status check_kv_cache_write(const void* k, int64_t ld_k, const void* v, int
                                  const int64_t* slot_mapping, int64_t T, int64_t H, int64_t D, int64_t num_slots,
                                  int mode, const float* k_scale, const float* v_scale, const void* k_cache,
                                  const void* v_cache);
+spec_status check_rms_norm(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, const void* weight,
+                           float eps, int64_t rows, int64_t cols, int mode, const float* scales, const void* q,
+                           int64_t ld_q, const void* sum, int64_t ld_sum, const void* y, int64_t ld_y);
+spec_status check_rope_kv_cache_write(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v,
+                                      int64_t ld_v, const int32_t* positions, const double* inv_freq, int64_t R,
+                                      int pairs, const int64_t* slot_mapping, int64_t T, int64_t Hq, int64_t H,
+                                      int64_t D, int64_t num_slots, int mode, const float* k_scale,
+                                      const float* v_scale, const void* k_cache, const void* v_cache,
+                                      const void* q_out, int64_t ld_q_out, const void* k_out, int64_t ld_k_out);
+spec_status check_fp4_quantize(const void* x, int64_t rows, int64_t cols, int64_t ld_x, const void* q, int64_t ld_q,
+                               const void* scales, int64_t ld_scales);
+spec_status check_gemm_fp4(const void* a, int64_t lda, const float* a_scale, int a_mode, const void* w, int64_t ldw,
+                           const void* w_scale, int64_t ld_w_scale, int64_t M, int64_t N, int64_t K, const void* y,
+                           int64_t ldy, int out_dtype);
 spec_status check_kv_cache_read(const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
                                 int mode, const int64_t* slot_mapping, int64_t T, int64_t H, int64_t D,
                                 int64_t num_slots, const void* k, int64_t ld_k, const void* v, int64_t ld_v);

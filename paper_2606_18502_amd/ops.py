@@ -54,6 +54,34 @@ def silu_mul(x: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tenso
     return (_bind or _load_bind()).silu_mul(x, out)
 
 
+def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5, residual: Optional[torch.Tensor] = None,
+             residual_out: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None
+             ) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Root-mean-square norm of bf16 rows, the residual added first (spec_fp8_rms_norm without codes).
+
+    x: bf16 [rows, cols]; weight: bf16 [cols]; residual: bf16 [rows, cols] or None.
+    Returns (out bf16 [rows, cols], residual_out = bf16(x + residual), or None where neither
+    residual nor residual_out is given).  out and residual_out may each be x or residual.
+    """
+    return (_bind or _load_bind()).rms_norm(x, weight, eps, residual, residual_out, out)
+
+
+def rms_norm_quantize(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5,
+                      residual: Optional[torch.Tensor] = None, per_tensor_scale: Optional[torch.Tensor] = None,
+                      residual_out: Optional[torch.Tensor] = None, normed: Optional[torch.Tensor] = None,
+                      out: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None
+                      ) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
+    """rms_norm with its result as E4M3 codes and scales, for the next linear (spec_fp8_rms_norm).
+
+    x, weight, residual, residual_out: as for rms_norm.  Dynamic per-row scales unless
+    `per_tensor_scale` (fp32 [1]) is given.  normed: bf16 [rows, cols] that also receives the
+    normed values, or None.
+    Returns (codes uint8 [rows, cols], scales fp32 [rows] or the given [1], residual_out or None).
+    """
+    return (_bind or _load_bind()).rms_norm_quantize(x, weight, eps, residual, per_tensor_scale, residual_out, normed, out,
+                                                     scales)
+
+
 def clip_count(x: torch.Tensor, scale: torch.Tensor, count: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Values of bf16 rows x that the static per-tensor scale clips (spec_fp8_clip_count):
     |fl32(x * fl32(1/scale))| > 448.  Accumulates into `count` (int64 [1]
@@ -74,6 +102,25 @@ def kv_cache_write(k: torch.Tensor, v: torch.Tensor, slot_mapping: torch.Tensor,
     written at the stored slots; per_tensor=True: fp32 [1], read.
     """
     (_bind or _load_bind()).kv_cache_write(k, v, slot_mapping, k_cache, v_cache, k_scale, v_scale, per_tensor)
+
+
+def rope_kv_cache_write(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor,
+                        inv_freq: torch.Tensor, slot_mapping: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                        k_scale: torch.Tensor, v_scale: torch.Tensor, per_tensor: bool = False,
+                        interleaved: bool = False, q_out: Optional[torch.Tensor] = None,
+                        k_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Rotate new queries and keys by their positions and write keys and values to the FP8 KV cache
+    (spec_fp8_rope_kv_cache_write).
+
+    q: bf16 [T, Hq, D]; k, v: bf16 [T, H, D] (views as kv_cache_write takes them, e.g. the column
+    blocks of the QKV output); positions: int32 [T]; inv_freq: fp64 [R/2], the angle of channel pair i
+    being positions * inv_freq[i]; channels from R on are not rotated.  Pairs are (i, i + R/2), or
+    (2i, 2i + 1) with interleaved.  slot_mapping, caches, scales, per_tensor: as for kv_cache_write.
+    q_out: bf16 [T, Hq, D] (may be q); k_out: bf16 [T, H, D] that also receives the rotated keys (may
+    be k; prompt_attention takes them), or None.  Returns q_out.
+    """
+    return (_bind or _load_bind()).rope_kv_cache_write(q, k, v, positions, inv_freq, slot_mapping, k_cache, v_cache, k_scale,
+                                                       v_scale, per_tensor, interleaved, q_out, k_out)
 
 
 def kv_cache_read(k_cache: torch.Tensor, v_cache: torch.Tensor, slot_mapping: torch.Tensor, k_scale: torch.Tensor,
@@ -151,6 +198,27 @@ def gemm(a: torch.Tensor, sa: torch.Tensor, w: torch.Tensor, sw: torch.Tensor,
     """
     f32 = True if out_dtype is torch.float32 else (False if out_dtype is torch.bfloat16 else None)
     return (_bind or _load_bind()).gemm(a, sa, w, sw, f32, out, workspace)
+
+
+def quantize_fp4(x: torch.Tensor, out: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None
+                 ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """MXFP4 of bf16 weights (spec_fp4_quantize): E2M1 codes, one E8M0 scale byte for 32 of them.
+
+    x: bf16 [N, K], K a multiple of 32.  Returns (codes uint8 [N, K/2], two a byte, the even column in
+    the low half; scales uint8 [N, K/32], 2^(byte - 127)).
+    """
+    return (_bind or _load_bind()).quantize_fp4(x, out, scales)
+
+
+def gemm_fp4(a: torch.Tensor, sa: torch.Tensor, w: torch.Tensor, sw: torch.Tensor,
+             out_dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Y = dec(A) dec4(W)^T * sa with 4-bit weights, for few rows (spec_fp8_gemm_fp4).
+
+    a: uint8 E4M3 [M, K]; sa: fp32 [M] (per token) or [1] (per tensor); w: uint8 [N, K/2] and
+    sw: uint8 [N, K/32] of quantize_fp4.  The weights are read once for every 64 rows of a.
+    """
+    f32 = True if out_dtype is torch.float32 else (False if out_dtype is torch.bfloat16 else None)
+    return (_bind or _load_bind()).gemm_fp4(a, sa, w, sw, f32, out)
 
 
 def gemm_silu_mul(a: torch.Tensor, sa: torch.Tensor, w: torch.Tensor, sw: torch.Tensor,
