@@ -88,6 +88,28 @@ def test_parity(M, N, K):
         check(y, p.gemm_fp4(d[0], one, d[2], d[3]), a, np.float32(0.03125), w, sw)
 
 
+@pytest.mark.parametrize("M", [3, 11, 27, 50])
+@pytest.mark.parametrize("N,K", [(70, 33056), (5000, 2080), (9000, 1184), (17000, 1312), (20000, 352), (33011, 4384), (4500, 16544),
+                                 (9000, 8320), (33011, 160)])
+def test_every_variant(M, N, K):
+    """Numbers of columns on all sides of the variants' borders, K beyond the scales that a workgroup holds at a time; sampled
+    columns, the first and last among them."""
+    p = need_gpu()
+    say(f"gemm_fp4 variants M={M} N={N} K={K}")
+    rng = np.random.default_rng(N + K)
+    a, sa = oq.quantize_rows(wl.linear_activations(M, K, 1, 0.01, 20.0))
+    w = rng.integers(0, 256, (N, K // 2), dtype=np.uint8)
+    sw = rng.integers(120, 128, (N, K // 32), dtype=np.uint8)
+    d = dev_u8(a), dev_f32(sa), dev_u8(w), dev_u8(sw)
+    cols = np.unique(np.concatenate((rng.choice(N, 40), np.arange(17), np.arange(N - 17, N))))
+    y32, y16 = p.gemm_fp4(*d, out_dtype=torch.float32), p.gemm_fp4(*d)
+    check(y32[:, cols].contiguous(), y16[:, cols].contiguous(), a, sa, w[cols], sw[cols])
+    # scales of any address: the same sums
+    odd = torch.zeros((N, K // 32 + 5), dtype=torch.uint8, device="cuda")
+    odd[:, 3:3 + K // 32] = d[3]
+    assert torch.equal(p.gemm_fp4(*d[:3], odd[:, 3:3 + K // 32], out_dtype=torch.float32), y32)
+
+
 def test_strides_and_what_lies_beside():
     p = need_gpu()
     M, N, K = 6, 90, 288
