@@ -150,7 +150,7 @@ spec_status spec_silu_mul_bf16(const void* x, int64_t rows, int64_t cols, int64_
  *         stride; sum and y not the same), and overlaps no input otherwise.
  * q       uint8 [rows, ld_q]; scales fp32 [rows] (PER_ROW) or [1] (PER_TENSOR; finite and > 0).
  * Requirements: rows >= 0 (0 is a no-op), cols > 0, every stride in use >= cols (SPEC_ERR_SHAPE);
- * cols % 8 == 0, cols <= 65536, rows < 2^31 (SPEC_ERR_UNSUPPORTED); 2^-60 <= eps < infinity
+ * cols % 8 == 0, cols <= 2^20, rows < 2^31 (SPEC_ERR_UNSUPPORTED); 2^-60 <= eps < infinity
  * (SPEC_ERR_VALUE); x, weight, one of q and y, and scales with q (SPEC_ERR_NULL); all of them 16-byte aligned, scales 4-byte,
  * strides multiples of 8 (SPEC_ERR_ALIGN); mode PER_ROW or PER_TENSOR (SPEC_ERR_ENUM).
  */

@@ -4,7 +4,10 @@
 // r = 1 / sqrt(mean h^2 + eps).  Because the product with r is last and rounding keeps order, the row's
 // largest |y| is fl32(max|h w| * r): the sum of squares and that maximum are reduced together, behind one barrier.
 //
-// One workgroup owns a row and keeps its sums in registers: every input is read once, every output written once.
+// One workgroup owns a row and keeps its sums in registers (rows of up to 32768 channels): every input is read once, every
+// output written once.  What bounds it: memory for many rows (8191 x 4096 with residual and codes 43 us, 5.5 TB/s of
+// 235 MB; a large copy runs at 5.1), a launch and two round trips for few (1 x 4096 3.1 us, of which 2.2 a launch).
+// 1000 x 65536 take 126 us (3.6 TB/s of what has to move): read twice.
 #pragma once
 
 #include "device_common.hpp"
@@ -44,88 +47,103 @@ __device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
     return o;
 }
 
-// NCH chunks of 8 channels per thread; chunk j of thread t is t + j * blockDim.x.
+// NCH > 0: NCH chunks of 8 channels per thread (chunk j of thread t is t + j * blockDim.x), loaded before any is used and
+// kept.  NCH == 0: rows too wide for registers; every pass reads x, the residual and the weights again, and the sum is
+// written in the last one, which may be where x or the residual lay.
 template <int NCH>
 __global__ __launch_bounds__(kNormMaxThreads) void rms_norm_kernel(NormArgs a) {
     __shared__ float red[32], red2[32];
     const int64_t row = blockIdx.x;
     const int chunks = a.cols / 8, t = threadIdx.x, nt = blockDim.x;
-    const uint16_t* const x = a.x + row * a.ld_x;
-    uint4 raw[NCH], add[NCH], wt[NCH];
-#pragma unroll
-    for (int j = 0; j < NCH; ++j) {
-        raw[j] = add[j] = wt[j] = uint4{0, 0, 0, 0};
-        if (t + j * nt < chunks) raw[j] = *reinterpret_cast<const uint4*>(x + (t + j * nt) * 8);
-    }
-    if (a.residual) {
-        const uint16_t* const r = a.residual + row * a.ld_r;
-#pragma unroll
-        for (int j = 0; j < NCH; ++j)
-            if (t + j * nt < chunks) add[j] = *reinterpret_cast<const uint4*>(r + (t + j * nt) * 8);
-    }
-#pragma unroll
-    for (int j = 0; j < NCH; ++j)
-        if (t + j * nt < chunks) wt[j] = *reinterpret_cast<const uint4*>(a.weight + (t + j * nt) * 8);
-
-    float h[NCH][8];
-    float sum = 0.0f, top = 0.0f;
-#pragma unroll
-    for (int j = 0; j < NCH; ++j) {
-        float w[8];
-        unpack8(raw[j], h[j]);
-        if (a.residual) {
+    const uint16_t *const x = a.x + row * a.ld_x, *const residual = a.residual ? a.residual + row * a.ld_r : nullptr;
+    const auto load = [](const uint16_t* p, int64_t c) { return *reinterpret_cast<const uint4*>(p + c * 8); };
+    const auto store_sum = [&](int64_t c, const float (&h)[8]) {
+        *reinterpret_cast<uint4*>(a.sum + row * a.ld_sum + c * 8) = pack8(h);
+    };
+    const auto add = [&](const uint4& raw, const uint4& more, float (&h)[8]) {
+        unpack8(raw, h);
+        if (residual) {
             float r[8];
-            unpack8(add[j], r);
+            unpack8(more, r);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) h[j][e] += r[e];
+            for (int e = 0; e < 8; ++e) h[e] += r[e];
         }
-        unpack8(wt[j], w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            sum = fmaf(h[j][e], h[j][e], sum);
-            top = fmaxf(top, fabsf(h[j][e] * w[e]));
-        }
-        if (a.sum && t + j * nt < chunks)
-            *reinterpret_cast<uint4*>(a.sum + row * a.ld_sum + (t + j * nt) * 8) = pack8(h[j]);
-    }
-    block_sum_max(sum, top, red);
-    const float cols = (float)a.cols;
-    float r = 1.0f / sqrtf(sum / cols + a.eps);
-    bool wild = false;                       // an infinite or NaN sum: the row is NaN throughout
-    if (sum < 0x1p126f && top < 0x1p126f) {
-        top *= r;
+    };
+    float h[NCH > 0 ? NCH : 1][8];
+    uint4 wt[NCH > 0 ? NCH : 1];
+    if constexpr (NCH > 0) {
+        uint4 raw[NCH], more[NCH];
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
-            float w[8];
-            unpack8(wt[j], w);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) h[j][e] = (h[j][e] * w[e]) * r;
+            raw[j] = more[j] = wt[j] = uint4{0, 0, 0, 0};
+            if (t + j * nt < chunks) raw[j] = load(x, t + j * nt);
         }
+        if (residual) {
+#pragma unroll
+            for (int j = 0; j < NCH; ++j)
+                if (t + j * nt < chunks) more[j] = load(residual, t + j * nt);
+        }
+#pragma unroll
+        for (int j = 0; j < NCH; ++j)
+            if (t + j * nt < chunks) wt[j] = load(a.weight, t + j * nt);
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            add(raw[j], more[j], h[j]);
+            if (a.sum && t + j * nt < chunks) store_sum(t + j * nt, h[j]);
+        }
+    }
+    // f(chunk, its sums, its weights) for this thread's chunks (a chunk behind the row's end: zeros)
+    const auto each = [&](auto f) {
+        float w[8];
+        if constexpr (NCH > 0) {
+#pragma unroll
+            for (int j = 0; j < NCH; ++j) {
+                unpack8(wt[j], w);
+                f(t + j * nt, h[j], w);
+            }
+        } else {
+#pragma unroll 2
+            for (int c = t; c < chunks; c += nt) {
+                add(load(x, c), residual ? load(residual, c) : uint4{0, 0, 0, 0}, h[0]);
+                unpack8(load(a.weight, c), w);
+                f(c, h[0], w);
+            }
+        }
+    };
+    float sum = 0.0f, top = 0.0f;
+    each([&](int, const float (&v)[8], const float (&w)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            sum = fmaf(v[e], v[e], sum);
+            top = fmaxf(top, fabsf(v[e] * w[e]));
+        }
+    });
+    block_sum_max(sum, top, red);
+    const float cols = (float)a.cols;
+    const bool plain = sum < 0x1p126f && top < 0x1p126f;
+    float r = 1.0f / sqrtf(sum / cols + a.eps), pre = 1.0f;
+    bool wild = false;                       // an infinite or NaN sum: the row is NaN throughout
+    if (plain) {
+        top *= r;
     } else {
         // Squares or products beyond fp32: squares of 2^-80 h (eps is nothing beside them), products with r first.
-        float pre = 1.0f, none = 0.0f;
+        float none = 0.0f;
         if (!(sum < 0x1p126f)) {
             pre = 0x1p-80f;
             sum = 0.0f;
+            each([&](int, const float (&v)[8], const float (&)[8]) {
 #pragma unroll
-            for (int j = 0; j < NCH; ++j)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum = fmaf(h[j][e] * pre, h[j][e] * pre, sum);
+                for (int e = 0; e < 8; ++e) sum = fmaf(v[e] * pre, v[e] * pre, sum);
+            });
             block_sum_max(sum, none, red2);
             wild = !(sum < INFINITY);
             r = 1.0f / sqrtf(sum / cols);
         }
-        top = 0.0f;
+        top = none = 0.0f;
+        each([&](int, const float (&v)[8], const float (&w)[8]) {
 #pragma unroll
-        for (int j = 0; j < NCH; ++j) {
-            float w[8];
-            unpack8(wt[j], w);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                h[j][e] = ((h[j][e] * pre) * r) * w[e];
-                top = fmaxf(top, fabsf(h[j][e]));
-            }
-        }
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(((v[e] * pre) * r) * w[e]));
+        });
         __syncthreads();                     // the first use of red
         block_sum_max(none, top, red);
     }
@@ -140,32 +158,37 @@ __global__ __launch_bounds__(kNormMaxThreads) void rms_norm_kernel(NormArgs a) {
         }
         inv = (float)(1.0 / (double)s);
     }
+    each([&](int c, const float (&v)[8], const float (&w)[8]) {
+        if (NCH > 0 && c >= chunks) return;
+        float y[8];
 #pragma unroll
-    for (int j = 0; j < NCH; ++j) {
-        const int c = t + j * nt;
-        if (c >= chunks) continue;
+        for (int e = 0; e < 8; ++e) y[e] = plain ? (v[e] * w[e]) * r : ((v[e] * pre) * r) * w[e];
+        if (NCH == 0 && a.sum) store_sum(c, v);
         if (a.y) {
-            uint4 o = pack8(h[j]);
+            uint4 o = pack8(y);
             if (wild) o = uint4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
-            *reinterpret_cast<uint4*>(a.y + row * a.ld_y + c * 8) = o;
+            *reinterpret_cast<uint4*>(a.y + row * a.ld_y + (int64_t)c * 8) = o;
         }
         if (a.q) {
             uint2 o;
-            o.x = e4m3x4(h[j][0] * inv, h[j][1] * inv, h[j][2] * inv, h[j][3] * inv);
-            o.y = e4m3x4(h[j][4] * inv, h[j][5] * inv, h[j][6] * inv, h[j][7] * inv);
+            o.x = e4m3x4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+            o.y = e4m3x4(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv);
             if (wild) o = uint2{0x7f7f7f7fu, 0x7f7f7f7fu};
-            *reinterpret_cast<uint2*>(a.q + row * a.ld_q + c * 8) = o;
+            *reinterpret_cast<uint2*>(a.q + row * a.ld_q + (int64_t)c * 8) = o;
         }
-    }
+    });
 }
 
 }  // namespace
 
 hipError_t launch_rms_norm(const NormArgs& a, hipStream_t stream) {
     const int chunks = a.cols / 8;
-    int threads = 256;
-    while (threads < kNormMaxThreads && chunks > 8 * threads) threads *= 2;
-    if (chunks < threads) threads = (chunks + kWave - 1) / kWave * kWave;
+    // One wave where two chunks a lane cover the row (no barrier), then up to four chunks a thread: 320 x 4096 4.1 us with
+    // 256 threads, 4.8 with 128, 4.2 with 512; 1005 x 7176 8.9 with 256, 9.9 with 512; 2000 x 16384 44.1 with 512, 52.5
+    // with 1024 (eight chunks in 256 threads spill: 79.6).
+    int threads = chunks <= 2 * kWave ? kWave : 256;
+    while (threads > kWave && threads < kNormMaxThreads && chunks > 4 * threads) threads *= 2;
+    if (threads > kWave && chunks < threads) threads = (chunks + kWave - 1) / kWave * kWave;
     const int64_t most = 1 << 21;            // rows of a launch (a grid's threads are counted in 32 bits)
     if (a.rows > most) {
         NormArgs part = a;
@@ -192,11 +215,8 @@ hipError_t launch_rms_norm(const NormArgs& a, hipStream_t stream) {
         SPEC_NORM_CASE(2)
         SPEC_NORM_CASE(3)
         SPEC_NORM_CASE(4)
-        SPEC_NORM_CASE(5)
-        SPEC_NORM_CASE(6)
-        SPEC_NORM_CASE(7)
         default:
-            hipLaunchKernelGGL(rms_norm_kernel<8>, grid, block, 0, stream, a);
+            hipLaunchKernelGGL(rms_norm_kernel<0>, grid, block, 0, stream, a);
     }
 #undef SPEC_NORM_CASE
     return hipGetLastError();

@@ -7,7 +7,7 @@
 
 namespace specfp8 {
 
-constexpr int64_t kNormMaxCols = 65536;      // of a norm's row: its sums stay in registers
+constexpr int64_t kNormMaxCols = 1 << 20;    // of a norm's row: a thread adds at most 1024 squares one after the other
 
 // ---- FP8 GEMM tiles ---------------------------------------------------------
 // A tile is a WM x WN grid of waves, each wave holding WTM x WTN blocks of
