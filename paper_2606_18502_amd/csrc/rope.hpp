@@ -9,6 +9,11 @@
 // token's R/2 angles once, one a lane, and hands them round through its corner of LDS.  G lanes own a row, 2 VEC
 // channels each: VEC of the lower and VEC of the upper half of the rotated channels, or 2 VEC side by side where
 // neighbours turn together and where nothing turns.
+//
+// What bounds it: memory for many tokens (8191 of 32 + 2 x 8 heads of 128, keys as bf16 too: 44.4 us, 4.5 TB/s of 202 MB;
+// a large copy runs at 5.1), a launch and three round trips for few (1 token 3.5 us, 320 4.4, of which 2.2 a launch).
+// Not faster there: the next rows loaded under this one's arithmetic (47.5), more waves a SIMD (45.4 and 52.8), workgroups of 2 or
+// 8 waves.  Stores past the caches gain 2 to 4 us here, and the attention that reads q next loses them.
 #pragma once
 
 #include "device_common.hpp"
@@ -164,7 +169,8 @@ hipError_t launch_rope_kv_write(const RopeArgs& given, bool interleaved, hipStre
     const int vec = wide ? 8 : 4;
     int g = 1;
     while (2 * vec * g < a.D) g *= 2;
-    // Parts of a token while the waves hardly fill the chip, each with some rows of its own.
+    // Parts of a token while the waves hardly fill the chip, each with some rows of its own (1024 tokens in two parts 7.2 us;
+    // 2048 in two 10.2, in one 10.9, but 2000 with heads of 256 12.1 and 10.5).
     const int64_t passes = ((int64_t)a.Hq + 2 * a.H) * g / kWave;
     a.log_parts = 0;
     while ((2LL << a.log_parts) <= passes && a.T << a.log_parts < 2048) ++a.log_parts;
