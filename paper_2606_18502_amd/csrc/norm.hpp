@@ -163,25 +163,29 @@ __global__ __launch_bounds__(kNormMaxThreads) void rms_norm_kernel(NormArgs a) {
         }
         inv = (float)(1.0 / (double)s);
     }
-    each([&](int c, const float (&v)[8], const float (&w)[8]) {
-        if (NCH > 0 && c >= chunks) return;
-        float y[8];
+    const auto finish = [&](auto value) {
+        each([&](int c, const float (&v)[8], const float (&w)[8]) {
+            if (NCH > 0 && c >= chunks) return;
+            float y[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = plain ? (v[e] * w[e]) * r : ((v[e] * pre) * r) * w[e];
-        if (NCH == 0 && a.sum) store_sum(c, v);
-        if (a.y) {
-            uint4 o = pack8(y);
-            if (wild) o = uint4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
-            *reinterpret_cast<uint4*>(a.y + row * a.ld_y + (int64_t)c * 8) = o;
-        }
-        if (a.q) {
-            uint2 o;
-            o.x = e4m3x4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
-            o.y = e4m3x4(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv);
-            if (wild) o = uint2{0x7f7f7f7fu, 0x7f7f7f7fu};
-            *reinterpret_cast<uint2*>(a.q + row * a.ld_q + (int64_t)c * 8) = o;
-        }
-    });
+            for (int e = 0; e < 8; ++e) y[e] = value(v[e], w[e]);
+            if (NCH == 0 && a.sum) store_sum(c, v);
+            if (a.y) {
+                uint4 o = pack8(y);
+                if (wild) o = uint4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+                *reinterpret_cast<uint4*>(a.y + row * a.ld_y + (int64_t)c * 8) = o;
+            }
+            if (a.q) {
+                uint2 o;
+                o.x = e4m3x4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+                o.y = e4m3x4(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv);
+                if (wild) o = uint2{0x7f7f7f7fu, 0x7f7f7f7fu};
+                *reinterpret_cast<uint2*>(a.q + row * a.ld_q + (int64_t)c * 8) = o;
+            }
+        });
+    };
+    if (plain) finish([&](float v, float w) { return (v * w) * r; });
+    else finish([&](float v, float w) { return ((v * pre) * r) * w; });
 }
 
 }  // namespace

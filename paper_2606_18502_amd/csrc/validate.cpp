@@ -137,7 +137,7 @@ spec_status check_gemm_fp4(const void* a, int64_t lda, const float* a_scale, int
     if (out_dtype != SPEC_OUT_BF16 && out_dtype != SPEC_OUT_F32) return SPEC_ERR_ENUM;
     if (M < 0 || N <= 0 || K <= 0) return SPEC_ERR_SHAPE;
     if (lda < K || ldw < K / 2 || ld_w_scale < K / 32 || ldy < N) return SPEC_ERR_SHAPE;
-    if (K % 32 != 0 || K > kMaxGrid || N >= 1LL << 28 || M > 16 * kMaxGridY) return SPEC_ERR_UNSUPPORTED;
+    if (K % 32 != 0 || K > 1LL << 30 || N >= 1LL << 28 || M > 16 * kMaxGridY) return SPEC_ERR_UNSUPPORTED;
     if (M == 0) return SPEC_OK;
     if (!a || !a_scale || !w || !w_scale || !y) return SPEC_ERR_NULL;
     if (lda % 16 != 0 || ldw % 16 != 0 || ldy % 8 != 0 || !aligned16(a) || !aligned16(w) || !aligned16(y))

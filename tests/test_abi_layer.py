@@ -118,7 +118,7 @@ def test_gemm_fp4(lib):
     assert gemm4(lib, out=2) == ENUM
     for bad in (dict(M=-1), dict(N=0), dict(K=0), dict(lda=496), dict(ldw=240), dict(ld_ws=15), dict(ldy=56)):
         assert gemm4(lib, **bad) == SHAPE, bad
-    for bad in (dict(K=496), dict(K=I31, lda=I31, ldw=I31, ld_ws=I31), dict(N=1 << 28, ldy=1 << 28), dict(M=1 << 20)):
+    for bad in (dict(K=496), dict(K=(1 << 30) + 32, lda=I31, ldw=I31, ld_ws=I31), dict(N=1 << 28, ldy=1 << 28), dict(M=1 << 20)):
         assert gemm4(lib, **bad) == UNSUP, bad
     for name in ("a", "sa", "w", "ws", "y"):
         assert gemm4(lib, **{name: None}) == NULL, name
