@@ -142,8 +142,8 @@ spec_status spec_silu_mul_bf16(const void* x, int64_t rows, int64_t cols, int64_
  * with spec_fp8_quantize's E4M3(.); the codes are of y in fp32, not of its bf16 rounding.  At
  * least one of q and y is given.  Sums are fp32, in an order that depends on cols alone.
  * A row whose h holds an infinity or a NaN has NaN for all of y, codes 0x7F and scale 2^-100;
- * finite rows stay finite also where their squares exceed fp32.  A weight that is not finite
- * gives unspecified codes.
+ * finite rows stay finite also where their squares exceed fp32.  Products h[c] * w[c] below 2^-126 lose bits.
+ * A weight that is not finite gives unspecified codes.
  *
  * x, residual  bf16 [rows, ld_x] / [rows, ld_residual]; weight bf16 [cols].
  * sum, y  bf16 [rows, ld_sum] / [rows, ld_y]; each may be x or residual itself (same pointer and

@@ -62,8 +62,9 @@ __global__ __launch_bounds__(256) void fp4_quantize_kernel(const uint16_t* __res
 // A go there without registers.  A step's operands are read from its stage under the products of the step before, and
 // the stage is loaded anew.  Scales, a 32nd of the operands' count, go there some thousand k at a time in 16-byte pieces:
 // a word a row and step, loaded with the stages, cost a fifth of 8 rows by 128256 x 4096.  Waves on their own wait for
-// their own loads; groups meet at a barrier a step.  Chunks of 16 bytes lie at slot c ^ f(row) of their row, so that the 16 lanes that an LDS cycle serves (lanes
-// l and l + 16, l % 16 < 8) hit different banks.
+// their own loads; groups meet at a barrier a step.  Two steps a stage (half the barriers) were within 5% at the shapes
+// with many steps and slower where they left a ring of two.  Chunks of 16 bytes lie at slot c ^ f(row) of their row, so
+// that the 16 lanes that an LDS cycle serves (lanes l and l + 16, l % 16 < 8) hit different banks.
 template <int MR, int NT, int KW, int NW, int D>
 struct Fp4Shape {
     static constexpr int MT = (MR + 15) / 16;                               // tiles of 16 rows of A

@@ -175,6 +175,22 @@ def test_more_rows_than_one_launch_takes():
         np.testing.assert_array_equal(host_bf16_bits(total[part]), wl.bf16_bits_from_f32(h.astype(np.float32)))
 
 
+def test_rows_beyond_32_bits():
+    """Row strides that put the second row past 2^31 elements, on every side."""
+    p = need_gpu()
+    cols, far = 264, 1 << 31
+    x, r, w = inputs(2, cols, 31)
+    box = torch.zeros(far + 4 * cols, dtype=torch.bfloat16, device="cuda")
+    dx, dr, ns, ny = (box.as_strided((2, cols), (far, 1), i * cols) for i in range(4))
+    codes = torch.zeros(far + cols, dtype=torch.uint8, device="cuda").as_strided((2, cols), (far, 1))
+    dx.copy_(dev_bf16(x))
+    dr.copy_(dev_bf16(r))
+    q, s, total = p.rms_norm_quantize(dx, dev_bf16(w), EPS, residual=dr, residual_out=ns, normed=ny, out=codes)
+    h = on.residual_sum(x, r)
+    check(on.rms_norm(h, w, EPS), q.contiguous(), s, ny.contiguous())
+    np.testing.assert_array_equal(host_bf16_bits(total.contiguous()), wl.bf16_bits_from_f32(h.astype(np.float32)))
+
+
 def test_refused_arguments_and_no_rows():
     p = need_gpu()
     d = dict(device="cuda")

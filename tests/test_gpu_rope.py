@@ -166,6 +166,22 @@ def test_an_empty_cache_and_no_tokens():
     assert got[0].shape == (0, Hq, D) and (got[2] == SENT_CODE).all()
 
 
+def test_a_cache_beyond_32_bits():
+    """Slots whose codes lie past 4 GiB: what is written there is what a small cache gets."""
+    p = need_gpu()
+    T, Hq, H, D = 4, 2, 2, 64
+    qkv, pos, freq, _ = make(T, Hq, H, D, D, 50, 17)
+    small = run(p, qkv, pos, freq, np.arange(T), Hq, H, D, T)
+    n = 2 ** 32 // (H * D) + 8
+    kc, vc = (torch.empty((n, H, D), dtype=torch.uint8, device="cuda") for _ in range(2))
+    ks, vs = (torch.empty((n, H), device="cuda") for _ in range(2))
+    slots = torch.tensor([n - 1, 2 ** 32 // (H * D), 2 ** 31 // (H * D), 0], device="cuda")
+    q, k, v = (dev_bf16(qkv)[:, a * D:b * D].unflatten(1, (b - a, D)) for a, b in ((0, Hq), (Hq, Hq + H), (Hq + H, Hq + 2 * H)))
+    p.rope_kv_cache_write(q, k, v, dev_i32(pos), torch.from_numpy(freq).cuda(), slots, kc, vc, ks, vs)
+    for a, b in zip(small[2:6], (kc, vc, ks, vs)):
+        assert torch.equal(a, b[slots])
+
+
 def test_a_row_of_zeros_and_the_plain_writes_scales():
     """A key of zeros has code 0 and the least scale; at position 0 nothing turns: keys are the plain write's, bit for bit."""
     p = need_gpu()
