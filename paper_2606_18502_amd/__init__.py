@@ -14,7 +14,11 @@ attention masks (tree_attention_mask), the FP8 KV-cache write of the new
 tokens' keys and values (kv_cache_write) and its reverse (kv_cache_read), the
 attention of new tokens, drafted chains and trees over that paged cache
 (paged_attention), and the causal attention of the packed prompts that fill it
-(prompt_attention).
+(prompt_attention).  Around the linears of a layer stand the root-mean-square
+norm with the residual's addition, into E4M3 codes (rms_norm_quantize, rms_norm),
+and the rotation of queries and keys on the way into the cache
+(rope_kv_cache_write); drafters, whose few rows are bound by reading weights,
+have linears with weights in 4 bits (quantize_fp4, gemm_fp4).
 
 The computation lives in libspecfp8.so (HIP kernels behind the C ABI of
 include/spec_fp8.h); this package only marshals torch tensors into that ABI.
@@ -27,6 +31,12 @@ A verify step, in outline (tensors on the GPU; shapes as in the docstrings):
     y = p.gemm(a_q, a_s, w_q, w_s)                # bf16 [M, N], fp32 accumulation
     h_q, h_s = p.quantize(y_gate_up, silu_mul=True)   # SiLU-gated input of the down projection
     out, num = p.verify_accept(target_logits, draft_logits, draft_tokens, uniforms, 0.7)
+
+A decoder layer's other calls, from the residual stream to the attention's input:
+
+    a_q, a_s, res = p.rms_norm_quantize(x, norm_w, residual=res)
+    qkv = p.gemm(a_q, a_s, w_q, w_s)                  # or p.gemm_fp4(a_q, a_s, *p.quantize_fp4(w_bf16))
+    q = p.rope_kv_cache_write(q, k, v, positions, inv_freq, slots, k_cache, v_cache, k_scale, v_scale)
 
 `out[b, :num[b] + 1]` are the tokens sequence b emits (accepted drafts, then
 the resampled or bonus token).  Static per-tensor scales: p.calibrate over
