@@ -360,7 +360,7 @@ spec_status spec_fp4_quantize(const void* x, int64_t rows, int64_t cols, int64_t
  * Y       bf16 or fp32 [M, ldy], N <= ldy.
  * Products are exact; the matrix cores' sums are those of spec_fp8_gemm.  The order of summation depends on N, K and M
  * alone.  No workspace.
- * Any M is computed, but weights are read once for every 64 rows: for many rows spec_fp8_gemm is made.
+ * Any M is computed, but at most 64 rows share a read of the weights: for many rows spec_fp8_gemm is made.
  * Requirements: M >= 0 (0 is a no-op), N > 0, K > 0, lda >= K, ldw >= K/2, ld_w_scale >= K/32, ldy >= N (SPEC_ERR_SHAPE);
  * K % 32 == 0, K <= 2^30, N < 2^28, M <= 2^20 - 16 (SPEC_ERR_UNSUPPORTED); A, W and Y 16-byte aligned, lda and ldw
  * multiples of 16, ldy of 8, a_scale 4-byte aligned (w_scale takes any stride and address) (SPEC_ERR_ALIGN).

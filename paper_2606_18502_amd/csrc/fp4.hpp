@@ -9,10 +9,10 @@
 // brings to them; of the activations' operand k 16 g .. and 64 + 16 g .. of a column.
 //
 // What bounds it: W's bytes.  8 rows by 128256 x 4096 take 51.7 us (5.4 TB/s of 279 MB; a read of a large array 5.8),
-// 5 by 4096 x 14336 7.4 and 1 by 6144 x 4096 4.9, of which 2.2 a launch.  With 64 rows A counts, too: every workgroup reads
-// all of it (64 by 28672 x 4096 15.0 us, 62 MB of W; 64 by 4096 x 14336 15.2 us, 235 MB of A to 29 of W), and from LDS
-// each wave.  Operands straight from memory to registers took 94, 11.6, 5.9 and 66 us: 16 rows a load instruction in
-// the matrix cores' order of lanes, and scales word by word.
+// 5 by 4096 x 14336 7.7 and 1 by 6144 x 4096 4.8, of which 2.2 a launch.  With 64 rows A counts, too: every workgroup
+// reads its rows of it (64 by 28672 x 4096 15.1 us, 62 MB of W; 64 by 4096 x 14336 11.8 us, 117 MB of A and 59 of W for
+// 29 in memory), and from LDS each wave.  Operands straight from memory to registers took 94, 11.6, 5.9 and 66 us for the
+// first four: 16 rows a load instruction in the matrix cores' order of lanes, and scales word by word.
 #pragma once
 
 #include <type_traits>
@@ -74,8 +74,8 @@ struct Fp4Shape {
     static constexpr int kLoadsA = MR / 8 / NW;                             // a wave's load instructions of a stage
     static constexpr int kLoads = NT + kLoadsA;
     static constexpr int kBox = KW > 1 ? KW * kTiles * MT * 1024 : 0;           // the waves' sums
-    static constexpr int kScales = KW * D * kStage;                         // of kPanel steps at a time: a word for each and row
-    static constexpr int kPanel = (kScales > 144000 ? 128 : 256) / (kTiles == 1 ? 1 : kTiles == 2 ? 2 : kTiles <= 4 ? 4 : 8);
+    static constexpr int kScales = KW * D * kStage;                         // of kPanel steps: a word for each and row
+    static constexpr int kPanel = 256 / (kTiles == 1 ? 1 : kTiles == 2 ? 2 : kTiles <= 4 ? 4 : 8);
     static constexpr int kPieces = (4 * kTiles * kPanel + kThreads - 1) / kThreads;         // of 16 bytes of scales a thread
     static constexpr int lds(int64_t steps) {
         const int ring = kScales + 16 * kTiles * 4 * ((int)(steps < kPanel ? steps : kPanel) | 1);
@@ -115,7 +115,13 @@ __global__ __launch_bounds__(64 * KW * NW) void gemm_fp4_kernel(Fp4Args a) {
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), r16 = lane & 15, g = lane >> 4;
     const int kw = wave / NW, nw = wave % NW;
-    const int64_t first_n = (int64_t)blockIdx.x * (16 * C::kTiles), n0 = first_n + 16 * NT * nw, m0 = (int64_t)blockIdx.y * MR;
+    // Workgroups go to the 8 XCDs in turn: those of further rows start so far into the columns that the ones that share
+    // columns of W, but for the last few, share an XCD's L2, too (24 by 3000 x 4096 4.9 us without, 4.3 with; 256 by
+    // 6000 x 14336 43.7, 38.3).
+    const unsigned across = (unsigned)((a.N + 16 * C::kTiles - 1) / (16 * C::kTiles));
+    unsigned tile = blockIdx.x + (across >= 8 ? across * blockIdx.y % 8 : 0);
+    if (tile >= across) tile -= across;
+    const int64_t first_n = (int64_t)tile * (16 * C::kTiles), n0 = first_n + 16 * NT * nw, m0 = (int64_t)blockIdx.y * MR;
     const int K = uniform((int)a.K), steps = K / 128;                       // whole ones
     uint8_t* const ring = smem + kw * (D * C::kStage);
     const uint32_t ring_at = uniform((int)lds_at(ring));
@@ -147,7 +153,8 @@ __global__ __launch_bounds__(64 * KW * NW) void gemm_fp4_kernel(Fp4Args a) {
         return i32x8_t{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
     };
     const int ar = MR == 8 ? r16 & 7 : r16;
-    const int w_at = NT * nw * 1024 + r16 * 64 + ((g ^ fp4_w_swizzle(r16)) << 4), a_at = C::kA + ar * 128 + ((g ^ fp4_a_swizzle(ar)) << 4);
+    const int w_at = NT * nw * 1024 + r16 * 64 + ((g ^ fp4_w_swizzle(r16)) << 4);
+    const int a_at = C::kA + ar * 128 + ((g ^ fp4_a_swizzle(ar)) << 4);
     for (int p0 = 0; p0 < steps; p0 += C::kPanel) {
         const int in_panel = min(steps - p0, C::kPanel);
         const int count = uniform((in_panel - kw + KW - 1) / KW);          // this wave's: kw, kw + KW, ..
@@ -278,7 +285,7 @@ __global__ __launch_bounds__(64 * KW * NW) void gemm_fp4_kernel(Fp4Args a) {
     // ---- a lane holds 4 outputs n of one row m
     const auto store = [&](int t, int x, f32x4_t v) {
         const int64_t m = m0 + 16 * x + r16, col = n0 + 16 * t + 4 * g;
-        if (m >= a.M || col >= a.N) return;
+        if (m >= a.M || col >= a.N || (MR == 8 && r16 >= 8)) return;        // (the other 8 are the first again)
         v *= a.a_scale[a.per_tensor ? 0 : m];
         if (a.out_f32) {
             float* const y = reinterpret_cast<float*>(a.y) + m * a.ldy + col;
@@ -333,35 +340,44 @@ hipError_t launch_fp4_quantize(const uint16_t* x, int64_t rows, int64_t cols, in
     return hipGetLastError();
 }
 
-// The variant, by the rows of A (8, 16, 32 or 64 a workgroup) and by the workgroups of 16 columns there would be.  Up to
-// one a compute unit, eight waves share K; more of them take more columns a workgroup, and 32 and 64 rows fewer waves
-// along K and more along the columns, which share A's tile: it is read by every workgroup, and weighs as much as W's
-// does with 16 columns and 8 rows.  Both sides of a border, us, K = 4096 (the variant before and after it):
-//   8 rows:  4096 columns 3.5, 3.6 -- 6144 5.2, 5.0;  10240 6.1, 6.4 -- 14336 7.4, 7.2, 128256 57.1, 51.7
-//   16:      4096 3.8, 4.8 -- 6144 5.7, 5.0;  8192 (D 3, D 2) 5.5, 5.7 -- 14336 7.4, 7.3;  14336 7.3, 8.1 -- 28672 12.2, 11.6
-//   32:      4096 4.6, 5.3 -- 6144 8.4, 5.8;  14336 8.3, 8.9 -- 28672 14.4, 12.5;  28672 12.5, 13.9 -- 128256 62.1, 57.5
-//   64:      4096 7.1, 6.8 (K = 14336: 15.2, 16.0) -- 6144 11.7, 7.3;  6144 7.3, 9.6 -- 10240 12.6, 9.5;
-//            14336 10.6, 11.6 -- 28672 19.2, 15.0;  28672 15.0, 17.2 -- 57344 39.4, 33.9
+// The variant, by the workgroups there would be.  Up to one a compute unit, eight waves share K, and a workgroup takes the
+// fewest rows that keep to that number, then two tiles of columns: it loads its rows of A and half as many bytes of its
+// columns of W, and few large ones leave compute units idle and load more each.  Beyond that 8 to 64 rows a workgroup
+// (they share a read of W), fewer waves along K and more along the columns, which share A's tile: it is read by every
+// workgroup, and weighs as much as W's does with 16 columns and 8 rows.  Both sides of a border, us, K = 4096 (14336 in
+// brackets; the variant before and after it):
+//   8 rows, 16:  16 by 2048 columns 3.5, 3.5 (6.2, 7.3) -- 4096 4.4, 3.9 (9.5, 8.1)
+//                32 by 1024 3.5, 3.5 (5.7, 6.7) -- 2048 4.4, 3.8 (8.5, 7.3)
+//   two tiles:   5 by 4096 3.4, 4.3 (7.6, 8.5) -- 6144 5.1, 4.7 (10.2, 9.8)
+//                32 by 2048 3.8, 3.9 (7.3, 8.8) -- 4096 5.0, 4.7 (11.1, 9.3)
+//   to 8 rows:   8192 5.5, 5.6 (11.7, 11.5) -- 10240 6.4, 6.0 (15.2, 13.5);  12288 6.5, 6.7 -- 28672 11.9, 11.3
+//   to 16:       8192 5.7, 6.4 (12.0, 14.2) -- 10240 7.0, 6.7 (17.9, 15.9);  16384 8.0, 8.6 -- 28672 12.2, 11.6
+//   to 32:       4096 4.7, 5.3 (9.3, 11.5) -- 6144 5.8, 5.5 (14.4, 12.3);  16384 8.5, 9.3 -- 28672 14.4, 12.5
+//                28672 12.5, 14.1 -- 128256 62.2, 57.8
+//   more:        2048 4.2, 4.7 (9.0, 11.0) -- 4096 5.7, 5.6 (14.3, 11.8);  4096 5.6, 6.8 (11.8, 16.1) -- 6144 7.4, 7.0
+//                8192 7.5, 9.4 -- 10240 13.0, 10.0;  16384 11.0, 11.9 -- 28672 19.1, 15.1;  28672 15.1, 17.2 -- 57344 39.6, 33.5
 hipError_t launch_gemm_fp4(const Fp4Args& a, hipStream_t stream) {
-    const int64_t tiles = (a.N + 15) / 16 * ((a.M + 63) / 64);
+    const int64_t columns = (a.N + 15) / 16;
+    const auto groups = [&](int rows, int64_t of_columns) { return (a.M + rows - 1) / rows * of_columns; };
+    if (groups(8, columns) <= 256) return launch_fp4_tiles<8, 1, 8, 1, 3>(a, stream);
+    if (groups(16, columns) <= 256) return launch_fp4_tiles<16, 1, 8, 1, 3>(a, stream);
+    if (groups(16, (columns + 1) / 2) <= 256)
+        return a.M <= 8 ? launch_fp4_tiles<8, 2, 8, 1, 2>(a, stream) : launch_fp4_tiles<16, 2, 8, 1, 2>(a, stream);
+    const int64_t tiles = groups(64, columns);
     if (a.M <= 8) {
-        if (tiles <= 256) return launch_fp4_tiles<8, 1, 8, 1, 3>(a, stream);
         if (tiles <= 768) return launch_fp4_tiles<8, 1, 4, 1, 3>(a, stream);
         return launch_fp4_tiles<8, 2, 4, 1, 2>(a, stream);
     }
     if (a.M <= 16) {
-        if (tiles <= 256) return launch_fp4_tiles<16, 1, 8, 1, 3>(a, stream);
-        if (tiles <= 512) return launch_fp4_tiles<16, 2, 4, 1, 3>(a, stream);
         if (tiles <= 1024) return launch_fp4_tiles<16, 2, 4, 1, 2>(a, stream);
         return launch_fp4_tiles<16, 4, 4, 1, 2>(a, stream);
     }
+    if (groups(32, (columns + 1) / 2) <= 256) return launch_fp4_tiles<32, 1, 4, 2, 3>(a, stream);
     if (a.M <= 32) {
-        if (tiles <= 256) return launch_fp4_tiles<32, 1, 8, 1, 3>(a, stream);
         if (tiles <= 1024) return launch_fp4_tiles<32, 1, 4, 2, 3>(a, stream);
         if (tiles <= 2048) return launch_fp4_tiles<32, 1, 2, 4, 3>(a, stream);
         return launch_fp4_tiles<32, 2, 1, 4, 3>(a, stream);
     }
-    if (tiles <= 256) return launch_fp4_tiles<64, 1, 8, 1, 2>(a, stream);
     if (tiles <= 512) return launch_fp4_tiles<64, 1, 4, 2, 3>(a, stream);
     if (tiles <= 1024) return launch_fp4_tiles<64, 1, 2, 4, 3>(a, stream);
     if (tiles <= 2048) return launch_fp4_tiles<64, 1, 1, 4, 3>(a, stream);

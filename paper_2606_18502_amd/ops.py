@@ -215,7 +215,7 @@ def gemm_fp4(a: torch.Tensor, sa: torch.Tensor, w: torch.Tensor, sw: torch.Tenso
     """Y = dec(A) dec4(W)^T * sa with 4-bit weights, for few rows (spec_fp8_gemm_fp4).
 
     a: uint8 E4M3 [M, K]; sa: fp32 [M] (per token) or [1] (per tensor); w: uint8 [N, K/2] and
-    sw: uint8 [N, K/32] of quantize_fp4.  The weights are read once for every 64 rows of a.
+    sw: uint8 [N, K/32] of quantize_fp4.  At most 64 rows of a share a read of the weights: for many rows, gemm.
     """
     f32 = True if out_dtype is torch.float32 else (False if out_dtype is torch.bfloat16 else None)
     return (_bind or _load_bind()).gemm_fp4(a, sa, w, sw, f32, out)
