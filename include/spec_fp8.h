@@ -249,7 +249,7 @@ spec_status spec_fp8_kv_cache_write(const void* k, int64_t ld_k, const void* v, 
  * positions int32 [T]; inv_freq fp64 [R/2], finite (of magnitude at most 1 or so: the angle is exact to 2^-52 of itself).
  * slot_mapping, num_slots, mode, k_scale, v_scale, k_cache, v_cache: as spec_fp8_kv_cache_write.
  * Requirements: those of spec_fp8_kv_cache_write; Hq >= 0, 0 < R <= D, ld_q and ld_q_out >= Hq*D, ld_k_out >= H*D
- * (SPEC_ERR_SHAPE); R % 8 == 0, Hq and H <= 65535 (SPEC_ERR_UNSUPPORTED); q, q_out and k_out 16-byte aligned, their strides
+ * (SPEC_ERR_SHAPE); R % 8 == 0, Hq and H <= 65535, strides < 2^35 (SPEC_ERR_UNSUPPORTED); q, q_out and k_out 16-byte aligned, their strides
  * multiples of 8, positions 4-byte and inv_freq 8-byte aligned (SPEC_ERR_ALIGN); pairs one of the two (SPEC_ERR_ENUM).
  * num_slots == 0 stores nothing: the caches and scales may be NULL.
  */

@@ -87,11 +87,11 @@ spec_status spec_fp8_rms_norm(const void* x, int64_t ld_x, const void* residual,
     a.ld_sum = ld_sum;
     a.ld_y = ld_y;
     a.ld_q = ld_q;
-    a.rows = rows;
     a.cols = (int32_t)cols;
+    a.threads = 0;
     a.per_tensor = mode == SPEC_SCALE_PER_TENSOR ? 1 : 0;
     a.eps = eps;
-    return from_hip(specfp8::launch_rms_norm(a, as_stream(stream)));
+    return from_hip(specfp8::launch_rms_norm(a, rows, as_stream(stream)));
 }
 
 spec_status spec_fp8_rope_kv_cache_write(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v,
@@ -130,7 +130,6 @@ spec_status spec_fp8_rope_kv_cache_write(const void* q, int64_t ld_q, const void
     a.D = (int32_t)D;
     a.R = (int32_t)R;
     a.per_tensor = mode == SPEC_SCALE_PER_TENSOR ? 1 : 0;
-    a.log_parts = 0;
     return from_hip(specfp8::launch_rope_kv_write(a, pairs == SPEC_ROPE_NEIGHBOURS, as_stream(stream)));
 }
 

@@ -36,6 +36,10 @@ SPEC_DEVICE_SIDE hipError_t launch_kv_cache_read(const uint8_t* k_cache, const u
                                                  int64_t T, int64_t H, int64_t D, int64_t num_slots, uint16_t* k,
                                                  int64_t ld_k, uint16_t* v, int64_t ld_v, hipStream_t stream);
 
+// A launch whose arguments, those that the compiler adds for blockDim and gridDim among them, take more bytes than this
+// costs the host 3.5 us, one of up to these 2.7 (the same kernel, queued among others).
+constexpr size_t kCheapArgs = 112;
+
 // ---- norm.hpp, in quantize.hip
 // Root-mean-square norm of rows ([rows][ld] bf16), the residual added first (or NULL); its sum, values and codes
 // (each or NULL) as include/spec_fp8.h states them.
@@ -44,11 +48,12 @@ struct NormArgs {
     uint16_t *sum, *y;
     uint8_t* q;
     float* scales;
-    int64_t ld_x, ld_r, ld_sum, ld_y, ld_q, rows;
-    int32_t cols, per_tensor;
+    int64_t ld_x, ld_r, ld_sum, ld_y, ld_q;
+    int32_t cols, threads, per_tensor;       // (threads: the launcher's)
     float eps;
 };
-SPEC_DEVICE_SIDE hipError_t launch_rms_norm(const NormArgs& a, hipStream_t stream);
+static_assert(sizeof(NormArgs) <= kCheapArgs, "a launch's cost");
+SPEC_DEVICE_SIDE hipError_t launch_rms_norm(const NormArgs& a, int64_t rows, hipStream_t stream);
 
 // ---- rope.hpp, in kvcache.hip
 // Queries and keys rotated by their positions; keys and values to the paged cache (include/spec_fp8.h).
@@ -61,7 +66,7 @@ struct RopeArgs {
     float *k_scale, *v_scale;
     uint8_t *k_cache, *v_cache;
     int64_t ld_q, ld_k, ld_v, ld_q_out, ld_k_out, T, num_slots;
-    int32_t Hq, H, D, R, per_tensor, log_parts;
+    int32_t Hq, H, D, R, per_tensor;
 };
 SPEC_DEVICE_SIDE hipError_t launch_rope_kv_write(const RopeArgs& a, bool interleaved, hipStream_t stream);
 

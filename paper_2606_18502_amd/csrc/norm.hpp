@@ -20,8 +20,8 @@ namespace {
 constexpr int kNormMaxThreads = 1024;
 
 // Sum and maximum over the block, combined in a fixed order; `red` holds 32 floats and is not in use.
-__device__ __forceinline__ void block_sum_max(float& sum, float& top, float* red) {
-    const int lane = threadIdx.x & (kWave - 1), w = threadIdx.x / kWave, nw = blockDim.x / kWave;
+__device__ __forceinline__ void block_sum_max(float& sum, float& top, float* red, int nw) {
+    const int lane = threadIdx.x & (kWave - 1), w = threadIdx.x / kWave;
     sum = wave_sum(sum);
     top = wave_max(top);
     if (nw == 1) return;
@@ -54,7 +54,7 @@ template <int NCH>
 __global__ __launch_bounds__(kNormMaxThreads) void rms_norm_kernel(NormArgs a) {
     __shared__ float red[32], red2[32];
     const int64_t row = blockIdx.x;
-    const int chunks = a.cols / 8, t = threadIdx.x, nt = blockDim.x;
+    const int chunks = a.cols / 8, t = threadIdx.x, nt = a.threads, nw = nt / kWave;
     const uint16_t *const x = a.x + row * a.ld_x, *const residual = a.residual ? a.residual + row * a.ld_r : nullptr;
     const auto load = [](const uint16_t* p, int64_t c) { return *reinterpret_cast<const uint4*>(p + c * 8); };
     // (past the caches: it is read when the layer's linears have run.  With 64 MB of other reads and its own behind it
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(kNormMaxThreads) void rms_norm_kernel(NormArgs a) {
             top = fmaxf(top, fabsf(v[e] * w[e]));
         }
     });
-    block_sum_max(sum, top, red);
+    block_sum_max(sum, top, red, nw);
     const float cols = (float)a.cols;
     const bool plain = sum < 0x1p126f && top < 0x1p126f;
     float r = 1.0f / sqrtf(sum / cols + a.eps), pre = 1.0f;
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(kNormMaxThreads) void rms_norm_kernel(NormArgs a) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum = fmaf(v[e] * pre, v[e] * pre, sum);
             });
-            block_sum_max(sum, none, red2);
+            block_sum_max(sum, none, red2, nw);
             wild = !(sum < INFINITY);
             r = 1.0f / sqrtf(sum / cols);
         }
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(kNormMaxThreads) void rms_norm_kernel(NormArgs a) {
             for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(((v[e] * pre) * r) * w[e]));
         });
         __syncthreads();                     // the first use of red
-        block_sum_max(none, top, red);
+        block_sum_max(none, top, red, nw);
     }
     float inv = 1.0f;
     if (a.q) {
@@ -190,7 +190,8 @@ __global__ __launch_bounds__(kNormMaxThreads) void rms_norm_kernel(NormArgs a) {
 
 }  // namespace
 
-hipError_t launch_rms_norm(const NormArgs& a, hipStream_t stream) {
+hipError_t launch_rms_norm(const NormArgs& given, int64_t rows, hipStream_t stream) {
+    NormArgs a = given;
     const int chunks = a.cols / 8;
     // One wave where two chunks a lane cover the row (no barrier), then up to four chunks a thread: 320 x 4096 4.1 us with
     // 256 threads, 4.8 with 128, 4.2 with 512; 1005 x 7176 8.9 with 256, 9.9 with 512; 2000 x 16384 44.1 with 512, 52.5
@@ -199,36 +200,32 @@ hipError_t launch_rms_norm(const NormArgs& a, hipStream_t stream) {
     while (threads > kWave && threads < kNormMaxThreads && chunks > 4 * threads) threads *= 2;
     if (threads > kWave && chunks < threads) threads = (chunks + kWave - 1) / kWave * kWave;
     const int64_t most = 1 << 21;            // rows of a launch (a grid's threads are counted in 32 bits)
-    if (a.rows > most) {
-        NormArgs part = a;
-        for (int64_t first = 0; first < a.rows; first += most) {
-            part.rows = a.rows - first < most ? a.rows - first : most;
-            part.x = a.x + first * a.ld_x;
-            if (a.residual) part.residual = a.residual + first * a.ld_r;
-            if (a.sum) part.sum = a.sum + first * a.ld_sum;
-            if (a.y) part.y = a.y + first * a.ld_y;
-            if (a.q) part.q = a.q + first * a.ld_q;
-            if (a.q && !a.per_tensor) part.scales = a.scales + first;
-            const hipError_t e = launch_rms_norm(part, stream);
-            if (e != hipSuccess) return e;
-        }
-        return hipSuccess;
-    }
-    const dim3 grid((unsigned)a.rows), block(threads);
+    a.threads = threads;
+    for (int64_t first = 0; first < rows; first += most) {
+        const dim3 grid((unsigned)(rows - first < most ? rows - first : most)), block(threads);
 #define SPEC_NORM_CASE(N)                                                               \
     case N:                                                                             \
         hipLaunchKernelGGL(rms_norm_kernel<N>, grid, block, 0, stream, a);              \
         break;
-    switch ((chunks + threads - 1) / threads) {
-        SPEC_NORM_CASE(1)
-        SPEC_NORM_CASE(2)
-        SPEC_NORM_CASE(3)
-        SPEC_NORM_CASE(4)
-        default:
-            hipLaunchKernelGGL(rms_norm_kernel<0>, grid, block, 0, stream, a);
-    }
+        switch ((chunks + threads - 1) / threads) {
+            SPEC_NORM_CASE(1)
+            SPEC_NORM_CASE(2)
+            SPEC_NORM_CASE(3)
+            SPEC_NORM_CASE(4)
+            default:
+                hipLaunchKernelGGL(rms_norm_kernel<0>, grid, block, 0, stream, a);
+        }
 #undef SPEC_NORM_CASE
-    return hipGetLastError();
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess || rows - first <= most) return e;
+        a.x += most * a.ld_x;
+        if (a.residual) a.residual += most * a.ld_r;
+        if (a.sum) a.sum += most * a.ld_sum;
+        if (a.y) a.y += most * a.ld_y;
+        if (a.q) a.q += most * a.ld_q;
+        if (a.q && !a.per_tensor) a.scales += most;
+    }
+    return hipSuccess;
 }
 
 }  // namespace specfp8

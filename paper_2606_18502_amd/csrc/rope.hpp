@@ -12,8 +12,8 @@
 //
 // What bounds it: memory for many tokens (8191 of 32 + 2 x 8 heads of 128, keys as bf16 too: 44.4 us, 4.5 TB/s of 202 MB;
 // a large copy runs at 5.1), a launch and three round trips for few (1 token 3.5 us, 320 4.4, of which 2.2 a launch).
-// Not faster there: the next rows loaded under this one's arithmetic (47.5), more waves a SIMD (45.4 and 52.8), workgroups of 2 or
-// 8 waves.  Stores past the caches gain 2 to 4 us here, and the attention that reads q next loses them.
+// Not faster there: the next rows loaded under this one's arithmetic (47.5), more waves a SIMD (45.4 and 52.8), workgroups
+// of 2 or 8 waves.  Stores past the caches gain 2 to 4 us here, and the attention that reads q next loses them.
 #pragma once
 
 #include "device_common.hpp"
@@ -25,6 +25,7 @@ namespace {
 
 constexpr int kRopeThreads = 256, kRopeWaves = kRopeThreads / kWave;
 constexpr int kRopeMaxPairs = 256;           // of a head (D <= 512)
+constexpr uint32_t kRopeMostBlocks = 1 << 22;
 
 // VEC (4 or 8) bf16 values
 template <int VEC>
@@ -40,6 +41,34 @@ struct RopeChunk {
     }
 };
 
+// The kernel's arguments, in no more bytes than a cheap launch has (a call that the host bounds takes 4.9 us with what
+// surrounds it, 5.15 with 176 bytes): addresses of 48 bits, which is what the GPU has of them, strides in eights of elements.
+enum RopePointer {
+    kQ, kK, kV, kQOut, kKOut, kPositions, kInvFreq, kSlots, kKScale, kVScale, kKCache, kVCache,
+    kRopePointers
+};
+struct RopeCall {
+    uint32_t low[kRopePointers];
+    uint16_t high[kRopePointers];
+    uint32_t ld[kKOut + 1];
+    uint32_t T;
+    int64_t num_slots;
+    uint16_t Hq, H;
+    uint8_t D8, R8, per_tensor : 1, log_parts : 7;
+
+    void set(RopePointer i, const void* p) {
+        low[i] = (uint32_t)reinterpret_cast<uintptr_t>(p);
+        high[i] = (uint16_t)(reinterpret_cast<uintptr_t>(p) >> 32);
+    }
+    template <class T>
+    __device__ __forceinline__ T* at(RopePointer i) const {
+        const uint64_t p = (uint64_t)high[i] << 32 | low[i];
+        return (T*)(__attribute__((address_space(1))) T*)p;      // (of global memory)
+    }
+    __device__ __forceinline__ int64_t stride(RopePointer i) const { return (int64_t)ld[i] * 8; }
+};
+static_assert(sizeof(RopeCall) <= kCheapArgs, "a launch's cost");
+
 // Angles of position `at`: cosine and sine of pair p at cs[p].
 __device__ __forceinline__ void rope_angles(int at, const double* inv_freq, int pairs, float2* cs) {
     for (int p = threadIdx.x & (kWave - 1); p < pairs; p += kWave) {
@@ -51,19 +80,18 @@ __device__ __forceinline__ void rope_angles(int at, const double* inv_freq, int 
 }
 
 template <int VEC, int G, bool INTERLEAVED>
-__global__ __launch_bounds__(kRopeThreads) void rope_kv_write_kernel(RopeArgs a) {
+__global__ __launch_bounds__(kRopeThreads) void rope_kv_write_kernel(RopeCall a) {
     __shared__ float2 angles[kRopeWaves][kRopeMaxPairs];
     const int lane = threadIdx.x & (kWave - 1), w = threadIdx.x / kWave;
     const int j = lane % G, sub = lane / G;
-    const int rows = a.Hq + 2 * a.H, D = a.D, step = (kWave / G) << a.log_parts;
-    const bool turns = 2 * VEC * j < a.R, mine = 2 * VEC * j < D;
-    const int64_t items = a.T << a.log_parts;
-    for (int64_t item = (int64_t)blockIdx.x * kRopeWaves + w; item < items; item += (int64_t)gridDim.x * kRopeWaves) {
+    const int Hq = a.Hq, H = a.H, D = 8 * a.D8, R = 8 * a.R8, rows = Hq + 2 * H, step = (kWave / G) << a.log_parts;
+    const bool turns = 2 * VEC * j < R, mine = 2 * VEC * j < D;
+    for (uint32_t item = blockIdx.x * kRopeWaves + w; item < a.T << a.log_parts; item += kRopeMostBlocks * kRopeWaves) {
         const int64_t t = item >> a.log_parts;
-        const int part = (int)(item & ((1 << a.log_parts) - 1));
-        const int64_t slot = a.slot[t];
+        const int part = (int)(item & ((1u << a.log_parts) - 1));
+        const int64_t slot = a.at<const int64_t>(kSlots)[t];
         const bool stored = slot >= 0 && slot < a.num_slots;
-        rope_angles(a.positions[t], a.inv_freq, a.R / 2, angles[w]);
+        rope_angles(a.at<const int32_t>(kPositions)[t], a.at<const double>(kInvFreq), R / 2, angles[w]);
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -75,19 +103,24 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kv_write_kernel(RopeArgs a)
             s[i] = cs.y;
         }
         __builtin_amdgcn_wave_barrier();     // (the next token's angles are written after these reads)
+        const uint16_t* const q_in = a.at<const uint16_t>(kQ) + t * a.stride(kQ);
+        const uint16_t* const k_in = a.at<const uint16_t>(kK) + t * a.stride(kK);
+        const uint16_t* const v_in = a.at<const uint16_t>(kV) + t * a.stride(kV);
+        uint16_t* const q_out = a.at<uint16_t>(kQOut) + t * a.stride(kQOut);
+        uint16_t* const k_out = a.at<uint16_t>(kKOut);
+        uint16_t* const k_row = k_out + t * a.stride(kKOut);
         for (int r0 = part * (kWave / G); r0 < rows; r0 += step) {
             const int r = r0 + sub;
             const bool live = mine && r < rows;
-            const int kind = r < a.Hq ? 0 : r < a.Hq + a.H ? 1 : 2;          // query, key, value
-            const int head = kind == 0 ? r : kind == 1 ? r - a.Hq : r - a.Hq - a.H;
+            const int kind = r < Hq ? 0 : r < Hq + H ? 1 : 2;                  // query, key, value
+            const int head = kind == 0 ? r : kind == 1 ? r - Hq : r - Hq - H;
             const bool halves = !INTERLEAVED && turns && kind != 2;
-            const int lo = halves ? VEC * j : 2 * VEC * j, hi = halves ? a.R / 2 + VEC * j : lo + VEC;
+            const int lo = halves ? VEC * j : 2 * VEC * j, hi = halves ? R / 2 + VEC * j : lo + VEC;
             float v[2 * VEC];
 #pragma unroll
             for (int i = 0; i < 2 * VEC; ++i) v[i] = 0.0f;
             if (live) {
-                const uint16_t* const src = (kind == 0 ? a.q + t * a.ld_q : kind == 1 ? a.k + t * a.ld_k : a.v + t * a.ld_v) +
-                                            (int64_t)head * D;
+                const uint16_t* const src = (kind == 0 ? q_in : kind == 1 ? k_in : v_in) + (int64_t)head * D;
                 RopeChunk<VEC> x, y;
                 x.load(src + lo);
                 y.load(src + hi);
@@ -109,9 +142,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kv_write_kernel(RopeArgs a)
                 }
             }
             if (kind != 2 && live) {
-                uint16_t* const out = kind == 0 ? a.q_out : a.k_out;
-                if (out) {
-                    uint16_t* const dst = out + t * (kind == 0 ? a.ld_q_out : a.ld_k_out) + (int64_t)head * D;
+                if (kind == 0 || k_out) {
+                    uint16_t* const dst = (kind == 0 ? q_out : k_row) + (int64_t)head * D;
                     RopeChunk<VEC> x, y;
 #pragma unroll
                     for (int i = 0; i < VEC / 2; ++i) {
@@ -122,15 +154,15 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kv_write_kernel(RopeArgs a)
                     y.store(dst + hi);
                 }
             }
-            if (!stored || r0 + kWave / G <= a.Hq) continue;                 // (the same in all lanes)
+            if (!stored || r0 + kWave / G <= Hq) continue;                   // (the same in all lanes)
             float amax = 0.0f;
 #pragma unroll
             for (int i = 0; i < 2 * VEC; ++i) amax = fmaxf(amax, fabsf(v[i]));
 #pragma unroll
             for (int o = G / 2; o >= 1; o /= 2) amax = fmaxf(amax, __shfl_xor(amax, o));
             if (kind == 0 || !live) continue;
-            float* const scale = kind == 1 ? a.k_scale : a.v_scale;
-            const int64_t at = slot * a.H + head;
+            float* const scale = kind == 1 ? a.at<float>(kKScale) : a.at<float>(kVScale);
+            const int64_t at = slot * H + head;
             float sc;
             if (a.per_tensor) {
                 sc = scale[0];
@@ -139,12 +171,13 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kv_write_kernel(RopeArgs a)
                 if (j == 0) scale[at] = sc;
             }
             const float inv = (float)(1.0 / (double)sc);
-            uint8_t* const dst = (kind == 1 ? a.k_cache : a.v_cache) + at * D;
+            uint8_t* const dst = (kind == 1 ? a.at<uint8_t>(kKCache) : a.at<uint8_t>(kVCache)) + at * D;
 #pragma unroll
             for (int i = 0; i < 2 * VEC; ++i) v[i] *= inv;
             if constexpr (VEC == 8) {
                 *reinterpret_cast<uint2*>(dst + lo) = uint2{e4m3x4(v[0], v[1], v[2], v[3]), e4m3x4(v[4], v[5], v[6], v[7])};
-                *reinterpret_cast<uint2*>(dst + hi) = uint2{e4m3x4(v[8], v[9], v[10], v[11]), e4m3x4(v[12], v[13], v[14], v[15])};
+                *reinterpret_cast<uint2*>(dst + hi) =
+                    uint2{e4m3x4(v[8], v[9], v[10], v[11]), e4m3x4(v[12], v[13], v[14], v[15])};
             } else {
                 *reinterpret_cast<uint32_t*>(dst + lo) = e4m3x4(v[0], v[1], v[2], v[3]);
                 *reinterpret_cast<uint32_t*>(dst + hi) = e4m3x4(v[4], v[5], v[6], v[7]);
@@ -154,17 +187,16 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kv_write_kernel(RopeArgs a)
 }
 
 template <int VEC, int G>
-void launch_rope_rows(const RopeArgs& a, bool interleaved, int64_t blocks, hipStream_t stream) {
+void launch_rope_rows(const RopeCall& a, bool interleaved, unsigned blocks, hipStream_t stream) {
     if (interleaved)
-        hipLaunchKernelGGL((rope_kv_write_kernel<VEC, G, true>), dim3((unsigned)blocks), dim3(kRopeThreads), 0, stream, a);
+        hipLaunchKernelGGL((rope_kv_write_kernel<VEC, G, true>), dim3(blocks), dim3(kRopeThreads), 0, stream, a);
     else
-        hipLaunchKernelGGL((rope_kv_write_kernel<VEC, G, false>), dim3((unsigned)blocks), dim3(kRopeThreads), 0, stream, a);
+        hipLaunchKernelGGL((rope_kv_write_kernel<VEC, G, false>), dim3(blocks), dim3(kRopeThreads), 0, stream, a);
 }
 
 }  // namespace
 
-hipError_t launch_rope_kv_write(const RopeArgs& given, bool interleaved, hipStream_t stream) {
-    RopeArgs a = given;
+hipError_t launch_rope_kv_write(const RopeArgs& a, bool interleaved, hipStream_t stream) {
     const bool wide = a.D % 16 == 0 && a.R % 16 == 0;          // 16-byte loads of both halves
     const int vec = wide ? 8 : 4;
     int g = 1;
@@ -172,13 +204,37 @@ hipError_t launch_rope_kv_write(const RopeArgs& given, bool interleaved, hipStre
     // Parts of a token while the waves hardly fill the chip, each with some rows of its own (1024 tokens in two parts 7.2 us;
     // 2048 in two 10.2, in one 10.9, but 2000 with heads of 256 12.1 and 10.5).
     const int64_t passes = ((int64_t)a.Hq + 2 * a.H) * g / kWave;
-    a.log_parts = 0;
-    while ((2LL << a.log_parts) <= passes && a.T << a.log_parts < 2048) ++a.log_parts;
-    int64_t blocks = ((a.T << a.log_parts) + kRopeWaves - 1) / kRopeWaves;
-    if (blocks > (1 << 24) - 1) blocks = (1 << 24) - 1;        // of fewer than 2^32 threads
-#define SPEC_ROPE_CASE(V, N)                                   \
-    case N:                                                    \
-        launch_rope_rows<V, N>(a, interleaved, blocks, stream); \
+    int log_parts = 0;
+    while ((2LL << log_parts) <= passes && a.T << log_parts < 2048) ++log_parts;
+    RopeCall c;
+    const int64_t strides[] = {a.ld_q, a.ld_k, a.ld_v, a.ld_q_out, a.ld_k_out};
+    for (int i = 0; i <= kKOut; ++i) c.ld[i] = (uint32_t)(strides[i] / 8);
+    c.num_slots = a.num_slots;
+    c.Hq = (uint16_t)a.Hq;
+    c.H = (uint16_t)a.H;
+    c.D8 = (uint8_t)(a.D / 8);
+    c.R8 = (uint8_t)(a.R / 8);
+    c.per_tensor = a.per_tensor != 0;
+    c.log_parts = log_parts;
+    c.T = (uint32_t)a.T;
+    c.set(kQ, a.q);
+    c.set(kK, a.k);
+    c.set(kV, a.v);
+    c.set(kQOut, a.q_out);
+    c.set(kKOut, a.k_out);
+    c.set(kPositions, a.positions);
+    c.set(kInvFreq, a.inv_freq);
+    c.set(kSlots, a.slot);
+    c.set(kKScale, a.k_scale);
+    c.set(kVScale, a.v_scale);
+    c.set(kKCache, a.k_cache);
+    c.set(kVCache, a.v_cache);
+    const uint32_t items = c.T << log_parts;
+    uint32_t blocks = (items + kRopeWaves - 1) / kRopeWaves;
+    if (blocks > kRopeMostBlocks) blocks = kRopeMostBlocks;
+#define SPEC_ROPE_CASE(V, N)                                    \
+    case N:                                                     \
+        launch_rope_rows<V, N>(c, interleaved, blocks, stream); \
         break;
     if (wide) {
         switch (g) {
@@ -188,7 +244,7 @@ hipError_t launch_rope_kv_write(const RopeArgs& given, bool interleaved, hipStre
             SPEC_ROPE_CASE(8, 8)
             SPEC_ROPE_CASE(8, 16)
             default:
-                launch_rope_rows<8, 32>(a, interleaved, blocks, stream);
+                launch_rope_rows<8, 32>(c, interleaved, blocks, stream);
         }
     } else {
         switch (g) {
@@ -199,7 +255,7 @@ hipError_t launch_rope_kv_write(const RopeArgs& given, bool interleaved, hipStre
             SPEC_ROPE_CASE(4, 16)
             SPEC_ROPE_CASE(4, 32)
             default:
-                launch_rope_rows<4, 64>(a, interleaved, blocks, stream);
+                launch_rope_rows<4, 64>(c, interleaved, blocks, stream);
         }
     }
 #undef SPEC_ROPE_CASE

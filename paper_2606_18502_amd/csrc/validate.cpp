@@ -109,6 +109,9 @@ spec_status check_rope_kv_cache_write(const void* q, int64_t ld_q, const void* k
                                                 empty ? v : v_cache);
     if (st == SPEC_ERR_ENUM || st == SPEC_ERR_SHAPE) return st;
     if (Hq > kMaxGridY || H > kMaxGridY) return SPEC_ERR_UNSUPPORTED;
+    constexpr int64_t far = 1LL << 35;       // the kernel holds strides in eights of elements, 32 bits of them
+    if ((Hq > 0 && (ld_q >= far || ld_q_out >= far)) || ld_k >= far || ld_v >= far || (k_out && ld_k_out >= far))
+        return SPEC_ERR_UNSUPPORTED;
     if (ld_q < Hq * D || (Hq > 0 && ld_q_out < Hq * D) || (k_out && ld_k_out < H * D)) return SPEC_ERR_SHAPE;
     if (st != SPEC_OK || T == 0) return st;
     if (!positions || !inv_freq || (Hq > 0 && (!q || !q_out))) return SPEC_ERR_NULL;

@@ -74,7 +74,8 @@ def test_rope_kv_cache_write(lib):
         assert rope(lib, **bad) == SHAPE, bad
     for bad in (dict(R=60), dict(D=100, R=96), dict(D=520, ld_q=1 << 15, ld_k=1 << 15, ld_v=1 << 15, ld_qo=1 << 15, ld_ko=1 << 15),
                 dict(T=I31), dict(Hq=65536, ld_q=1 << 24, ld_qo=1 << 24),
-                dict(H=65536, ld_k=1 << 24, ld_v=1 << 24, ld_ko=1 << 24)):
+                dict(H=65536, ld_k=1 << 24, ld_v=1 << 24, ld_ko=1 << 24),
+                *(dict([(name, 1 << 35)]) for name in ("ld_q", "ld_k", "ld_v", "ld_qo", "ld_ko"))):
         assert rope(lib, **bad) == UNSUP, bad
     for name in ("q", "k", "v", "pos", "freq", "slots", "ks", "vs", "kc", "vc", "qo"):
         assert rope(lib, **{name: None}) == NULL, name

@@ -182,6 +182,26 @@ def test_a_cache_beyond_32_bits():
         assert torch.equal(a, b[slots])
 
 
+def test_more_tokens_than_one_grid_covers():
+    p = need_gpu()
+    T, D, last = 2 ** 24 + 5, 8, 9
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn((T, D), device="cuda", generator=g).to(torch.bfloat16)[:, None]
+    pos = (torch.arange(T, device="cuda", dtype=torch.int64) % 5000).to(torch.int32)
+    freq = torch.tensor([1.0, 0.3, 0.07, 0.001], dtype=torch.float64, device="cuda")
+    slots = torch.full((T,), -1, device="cuda")
+    slots[-last:] = torch.arange(last, device="cuda")
+
+    def call(first):
+        kc = torch.full((last, 1, D), SENT_CODE, dtype=torch.uint8, device="cuda")
+        ks = torch.full((last, 1), SENT_SCALE, device="cuda")
+        vc, vs, t = kc.clone(), ks.clone(), x[first:]
+        return p.rope_kv_cache_write(t, t, t, pos[first:], freq, slots[first:], kc, vc, ks, vs)[-last:], kc, vc, ks, vs
+
+    for a, b in zip(call(0), call(T - last)):
+        assert torch.equal(a, b)
+
+
 def test_a_row_of_zeros_and_the_plain_writes_scales():
     """A key of zeros has code 0 and the least scale; at position 0 nothing turns: keys are the plain write's, bit for bit."""
     p = need_gpu()
