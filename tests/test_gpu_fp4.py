@@ -89,7 +89,7 @@ def test_parity(M, N, K):
 
 
 @pytest.mark.parametrize("M", [3, 11, 27, 50])
-@pytest.mark.parametrize("N,K", [(70, 33056), (1300, 33056), (2500, 33056), (5000, 2080), (9000, 1184), (17000, 1312), (20000, 352), (33011, 4384), (4500, 16544),
+@pytest.mark.parametrize("N,K", [(70, 33056), (1300, 33056), (2500, 33056), (5000, 2080), (9000, 1184), (14000, 2080), (17000, 1312), (20000, 352), (33011, 4384), (4500, 16544),
                                  (9000, 8320), (33011, 160)])
 def test_every_variant(M, N, K):
     """Numbers of columns on all sides of the variants' borders, K beyond the scales that a workgroup holds at a time; sampled
