@@ -10,7 +10,7 @@
 // channels each: VEC of the lower and VEC of the upper half of the rotated channels, or 2 VEC side by side where
 // neighbours turn together and where nothing turns.
 //
-// What bounds it: memory for many tokens (8191 of 32 + 2 x 8 heads of 128, keys as bf16 too: 44.4 us, 4.5 TB/s of 202 MB;
+// What bounds it: memory for many tokens (8191 of 32 + 2 x 8 heads of 128, keys as bf16 too: 43.8 us, 4.6 TB/s of 202 MB;
 // a large copy runs at 5.1), a launch and three round trips for few (1 token 3.5 us, 320 4.4, of which 2.2 a launch).
 // Not faster there: the next rows loaded under this one's arithmetic (47.5), more waves a SIMD (45.4 and 52.8), workgroups
 // of 2 or 8 waves.  Stores past the caches gain 2 to 4 us here, and the attention that reads q next loses them.
@@ -201,11 +201,13 @@ hipError_t launch_rope_kv_write(const RopeArgs& a, bool interleaved, hipStream_t
     const int vec = wide ? 8 : 4;
     int g = 1;
     while (2 * vec * g < a.D) g *= 2;
-    // Parts of a token while the waves hardly fill the chip, each with some rows of its own (1024 tokens in two parts 7.2 us;
-    // 2048 in two 10.2, in one 10.9, but 2000 with heads of 256 12.1 and 10.5).
+    // Parts of a token, each with some passes of its own, while all waves are resident (four a SIMD): 2048 tokens of 32 + 2 x 8
+    // heads of 128 in two 10.2 us, in one 10.8; 2500 13.3, 12.3.  Two for long work, too, whose waves then end more evenly:
+    // 8191 tokens 40.4, 41.0 (neighbours 39.7, 42.3), 4096 with heads of 256 40.1, 43.0; 4096 with heads of 128 19.5, 18.8.
     const int64_t passes = ((int64_t)a.Hq + 2 * a.H) * g / kWave;
     int log_parts = 0;
-    while ((2LL << log_parts) <= passes && a.T << log_parts < 2048) ++log_parts;
+    while ((2LL << log_parts) <= passes && a.T << log_parts <= 2048) ++log_parts;
+    if (log_parts == 0 && passes >= 6 && a.T * passes > 40000) log_parts = 1;
     RopeCall c;
     const int64_t strides[] = {a.ld_q, a.ld_k, a.ld_v, a.ld_q_out, a.ld_k_out};
     for (int i = 0; i <= kKOut; ++i) c.ld[i] = (uint32_t)(strides[i] / 8);

@@ -73,7 +73,7 @@ def check(y32, y16, a, sa, codes, scales):
 @pytest.mark.parametrize("M,N,K", [
     (1, 1, 32), (1, 64, 4096), (2, 33, 64), (3, 100, 96), (5, 200, 160), (7, 65, 480), (8, 256, 512), (9, 250, 544), (15, 31, 1024),
     (16, 48, 2080), (17, 130, 2048), (31, 96, 1056), (33, 96, 4096), (48, 40, 992), (63, 72, 1536), (64, 128, 4096), (65, 40, 576),
-    (130, 24, 672), (1, 512, 14336), (4, 96, 14336), (12, 1000, 736), (130, 1000, 96), (200, 4500, 288),
+    (130, 24, 672), (1, 512, 14336), (4, 96, 14336), (12, 1000, 736), (130, 1000, 96), (200, 4500, 288), (150, 12000, 96),
 ])
 def test_parity(M, N, K):
     p = need_gpu()
