@@ -131,7 +131,7 @@ __global__ __launch_bounds__(kNormMaxThreads) void rms_norm_kernel(NormArgs a) {
     if (plain) {
         top *= r;
     } else {
-        // Squares or products beyond fp32: squares of 2^-80 h (eps is nothing beside them), products with r first.
+        // Squares or products beyond fp32: squares of 2^-80 h (and eps 2^-160 beside their mean), products with r first.
         float none = 0.0f;
         if (!(sum < 0x1p126f)) {
             pre = 0x1p-80f;
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(kNormMaxThreads) void rms_norm_kernel(NormArgs a) {
             });
             block_sum_max(sum, none, red2, nw);
             wild = !(sum < INFINITY);
-            r = 1.0f / sqrtf(sum / cols);
+            r = 1.0f / sqrtf(sum / cols + a.eps * pre * pre);
         }
         top = none = 0.0f;
         each([&](int, const float (&v)[8], const float (&w)[8]) {

@@ -222,3 +222,20 @@ def test_refused_arguments_and_no_rows():
     y, total = p.rms_norm(x, w, residual_out=torch.empty_like(x))
     assert torch.equal(total, x)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("cols", [4096, 40000])
+def test_an_eps_of_the_size_of_the_squares(cols):
+    """Rows on both sides of 2^126, what their squares sum to, under an eps as large as their mean: it counts on either side."""
+    p = need_gpu()
+    rows = 6
+    x = wl.f32_from_bf16_bits(inputs(rows, cols, 13, False)[0]).copy()
+    x /= np.sqrt(np.mean(x.astype(np.float64) ** 2, axis=1, keepdims=True)).astype(np.float32)
+    mean = 2.0 ** 126 / cols * np.array([0.25, 0.9, 1.1, 4.0, 16.0, 4096.0])
+    x = wl.bf16_bits_from_f32(x * np.sqrt(mean)[:, None].astype(np.float32))
+    w = inputs(1, cols, 14)[2]
+    for eps in (2.0 ** 126 / cols, 2.0 ** 126):
+        y = on.rms_norm(on.residual_sum(x), w, eps)
+        ny = torch.empty((rows, cols), dtype=torch.bfloat16, device="cuda")
+        q, s, _ = p.rms_norm_quantize(dev_bf16(x), dev_bf16(w), eps, normed=ny)
+        check(y, q, s, ny)
