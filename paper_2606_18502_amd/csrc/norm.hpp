@@ -125,15 +125,16 @@ __global__ __launch_bounds__(kNormMaxThreads) void rms_norm_kernel(NormArgs a) {
     });
     block_sum_max(sum, top, red, nw);
     const float cols = (float)a.cols;
-    const bool plain = sum < 0x1p126f && top < 0x1p126f;
     float r = 1.0f / sqrtf(sum / cols + a.eps), pre = 1.0f;
+    const bool fits = sum < 0x1p126f && r > 0.0f;            // (r = 0: the mean with an eps near the largest number)
+    const bool plain = fits && top < 0x1p126f;
     bool wild = false;                       // an infinite or NaN sum: the row is NaN throughout
     if (plain) {
         top *= r;
     } else {
         // Squares or products beyond fp32: squares of 2^-80 h (and eps 2^-160 beside their mean), products with r first.
         float none = 0.0f;
-        if (!(sum < 0x1p126f)) {
+        if (!fits) {
             pre = 0x1p-80f;
             sum = 0.0f;
             each([&](int, const float (&v)[8], const float (&)[8]) {

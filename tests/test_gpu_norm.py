@@ -239,3 +239,16 @@ def test_an_eps_of_the_size_of_the_squares(cols):
         ny = torch.empty((rows, cols), dtype=torch.bfloat16, device="cuda")
         q, s, _ = p.rms_norm_quantize(dev_bf16(x), dev_bf16(w), eps, normed=ny)
         check(y, q, s, ny)
+
+
+def test_an_eps_near_the_largest_number():
+    """The mean of the squares and eps together exceed fp32, although neither does."""
+    p = need_gpu()
+    eps = float(np.finfo(np.float32).max)
+    x = wl.bf16_bits_from_f32(np.outer([3e18, 1.0, 1e30], [1, -1, 0.5, 0.25, -1, 1, 0.75, 1]).astype(np.float32))
+    w = inputs(1, 8, 16)[2]
+    y = on.rms_norm(on.residual_sum(x), w, eps)
+    assert (np.abs(y[0]) > 0.01).all()
+    ny = torch.empty((3, 8), dtype=torch.bfloat16, device="cuda")
+    q, s, _ = p.rms_norm_quantize(dev_bf16(x), dev_bf16(w), eps, normed=ny)
+    check(y, q, s, ny)
