@@ -129,10 +129,11 @@ __global__ __launch_bounds__(kNormMaxThreads) void rms_norm_kernel(NormArgs a) {
     const bool fits = sum < 0x1p126f && r > 0.0f;            // (r = 0: the mean with an eps near the largest number)
     const bool plain = fits && top < 0x1p126f;
     bool wild = false;                       // an infinite or NaN sum: the row is NaN throughout
+    const auto far = [&](float v, float w) { return (float)((double)v * w * ((double)r * pre)); };
     if (plain) {
         top *= r;
     } else {
-        // Squares or products beyond fp32: squares of 2^-80 h (and eps 2^-160 beside their mean), products with r first.
+        // Squares or products beyond fp32: squares of 2^-80 h (and eps 2^-160 beside their mean), y from 64 bits.
         float none = 0.0f;
         if (!fits) {
             pre = 0x1p-80f;
@@ -148,7 +149,7 @@ __global__ __launch_bounds__(kNormMaxThreads) void rms_norm_kernel(NormArgs a) {
         top = none = 0.0f;
         each([&](int, const float (&v)[8], const float (&w)[8]) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(((v[e] * pre) * r) * w[e]));
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(far(v[e], w[e])));
         });
         __syncthreads();                     // the first use of red
         block_sum_max(none, top, red, nw);
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(kNormMaxThreads) void rms_norm_kernel(NormArgs a) {
         });
     };
     if (plain) finish([&](float v, float w) { return (v * w) * r; });
-    else finish([&](float v, float w) { return ((v * pre) * r) * w; });
+    else finish(far);
 }
 
 }  // namespace

@@ -252,3 +252,22 @@ def test_an_eps_near_the_largest_number():
     ny = torch.empty((3, 8), dtype=torch.bfloat16, device="cuda")
     q, s, _ = p.rms_norm_quantize(dev_bf16(x), dev_bf16(w), eps, normed=ny)
     check(y, q, s, ny)
+
+
+@pytest.mark.parametrize("cols", [512, 40000])
+def test_small_channels_beside_large_ones(cols):
+    """A channel whose square exceeds fp32, and channels down to 2^-66 with weights of 2^-3 to 2^40 beside it: y keeps its bits down
+    to the least normal number."""
+    p = need_gpu()
+    rows = 4
+    x = wl.f32_from_bf16_bits(inputs(rows, cols, 17, False)[0]).astype(np.float64)
+    x = np.copysign(1 + np.abs(x) % 1, x) * 2.0 ** -np.linspace(30, 66, cols)
+    x[:, 5], x[1, 7] = 2.0 ** 66, 2.0 ** 70
+    x = wl.bf16_bits_from_f32(x.astype(np.float32))
+    w = wl.bf16_bits_from_f32((2.0 ** (np.arange(cols) % 44 - 3)).astype(np.float32))
+    y = on.rms_norm(on.residual_sum(x), w, EPS)
+    normal = np.abs(y) >= 2.0 ** -126
+    assert (normal & (np.abs(y) < 2.0 ** -110)).sum() > rows * 20
+    ny = torch.empty((rows, cols), dtype=torch.bfloat16, device="cuda")
+    q, s, _ = p.rms_norm_quantize(dev_bf16(x), dev_bf16(w), EPS, normed=ny)
+    check(y, q, s, ny)
