@@ -108,7 +108,7 @@ spec_status check_rope_kv_cache_write(const void* q, int64_t ld_q, const void* k
                                                 empty && !v_scale ? &unused : v_scale, empty ? k : k_cache,
                                                 empty ? v : v_cache);
     if (st == SPEC_ERR_ENUM || st == SPEC_ERR_SHAPE) return st;
-    if (Hq > kMaxGridY || H > kMaxGridY) return SPEC_ERR_UNSUPPORTED;
+    if (Hq > kMaxGridY || H > kMaxGridY || D > 512) return SPEC_ERR_UNSUPPORTED;    // (before their products)
     constexpr int64_t far = 1LL << 35;       // the kernel holds strides in eights of elements, 32 bits of them
     if ((Hq > 0 && (ld_q >= far || ld_q_out >= far)) || ld_k >= far || ld_v >= far || (k_out && ld_k_out >= far))
         return SPEC_ERR_UNSUPPORTED;

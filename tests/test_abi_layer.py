@@ -168,3 +168,11 @@ def test_the_refusals_under_sanitizers(tmp_path):
     log = res.stdout + res.stderr
     assert res.returncode == 0, log[-4000:]
     assert "ERROR: AddressSanitizer" not in log and "runtime error:" not in log, log[-4000:]
+
+
+def test_sizes_whose_products_exceed_64_bits(lib):
+    """Refused by the heads' size alone, before any stride is compared with a product (the sanitized run sees an overflow)."""
+    for D in (1 << 60, 1 << 62, (1 << 63) - 8):
+        for far in ({}, dict.fromkeys(("ld_q", "ld_k", "ld_v", "ld_qo", "ld_ko"), (1 << 63) - 8)):
+            assert rope(lib, D=D, **far) == UNSUP, (D, far)
+            assert rope(lib, D=D, R=D, Hq=1, H=1, **far) == UNSUP, (D, far)
