@@ -97,6 +97,21 @@ constexpr int64_t kAcceptSlice = (int64_t)64 * kAcceptVecs * 8;          // 4096
 constexpr int kAcceptPerThread = kAcceptVecs * 8;                        // 64 logits per thread (sampling)
 constexpr int64_t kAcceptChunk = (int64_t)kAcceptThreads * kAcceptPerThread;   // 16384 logits per sampling block
 
+// ---- rotation into the cache ----------------------------------------------------
+constexpr int64_t kRopeStep = 1 << 24;       // items (parts of tokens) that a grid's waves take at a time, counted in 32 bits
+
+// log2 of a token's parts, each with some passes of its own over rows of g lanes, while all waves are resident (four a
+// SIMD): 2048 tokens of 32 + 2 x 8 heads of 128 in two 10.2 us, in one 10.8; 2500 13.3, 12.3.  Two for long work, too,
+// whose waves then end more evenly: 8191 tokens 40.4, 41.0 (neighbours 39.7, 42.3), 4096 with heads of 256 40.1, 43.0;
+// 4096 with heads of 128 19.5, 18.8.  Not where a step past the last part would exceed 32 bits.
+inline int rope_log_parts(int64_t T, int64_t Hq, int64_t H, int g) {
+    const int64_t passes = (Hq + 2 * H) * g / 64;
+    int log_parts = 0;
+    while ((2LL << log_parts) <= passes && T << log_parts <= 2048) ++log_parts;
+    if (log_parts == 0 && passes >= 6 && T * passes > 40000 && 2 * T + kRopeStep <= 1LL << 32) log_parts = 1;
+    return log_parts;
+}
+
 // ---- paged attention ----------------------------------------------------------
 constexpr size_t kAttnTicketBytes = 16384;   // at the start of the workspace, zero between calls
 

@@ -18,6 +18,7 @@
 
 #include "device_common.hpp"
 #include "kernels.hpp"
+#include "plan.hpp"
 
 namespace specfp8 {
 
@@ -25,7 +26,7 @@ namespace {
 
 constexpr int kRopeThreads = 256, kRopeWaves = kRopeThreads / kWave;
 constexpr int kRopeMaxPairs = 256;           // of a head (D <= 512)
-constexpr uint32_t kRopeMostBlocks = 1 << 22;
+constexpr uint32_t kRopeMostBlocks = kRopeStep / kRopeWaves;
 
 // VEC (4 or 8) bf16 values
 template <int VEC>
@@ -201,13 +202,7 @@ hipError_t launch_rope_kv_write(const RopeArgs& a, bool interleaved, hipStream_t
     const int vec = wide ? 8 : 4;
     int g = 1;
     while (2 * vec * g < a.D) g *= 2;
-    // Parts of a token, each with some passes of its own, while all waves are resident (four a SIMD): 2048 tokens of 32 + 2 x 8
-    // heads of 128 in two 10.2 us, in one 10.8; 2500 13.3, 12.3.  Two for long work, too, whose waves then end more evenly:
-    // 8191 tokens 40.4, 41.0 (neighbours 39.7, 42.3), 4096 with heads of 256 40.1, 43.0; 4096 with heads of 128 19.5, 18.8.
-    const int64_t passes = ((int64_t)a.Hq + 2 * a.H) * g / kWave;
-    int log_parts = 0;
-    while ((2LL << log_parts) <= passes && a.T << log_parts <= 2048) ++log_parts;
-    if (log_parts == 0 && passes >= 6 && a.T * passes > 40000) log_parts = 1;
+    const int log_parts = rope_log_parts(a.T, a.Hq, a.H, g);
     RopeCall c;
     const int64_t strides[] = {a.ld_q, a.ld_k, a.ld_v, a.ld_q_out, a.ld_k_out};
     for (int i = 0; i <= kKOut; ++i) c.ld[i] = (uint32_t)(strides[i] / 8);
