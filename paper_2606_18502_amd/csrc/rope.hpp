@@ -70,12 +70,16 @@ struct RopeCall {
 };
 static_assert(sizeof(RopeCall) <= kCheapArgs, "a launch's cost");
 
-// Angles of position `at`: cosine and sine of pair p at cs[p].
+// Angles of position `at`: cosine and sine of pair p at cs[p].  inv_freq / 2 pi is held in two parts and the product's whole
+// turns are taken off inside a fused operation, so that the rest of a turn is off by some 2^-54 turns at every position (with
+// one part by 2^-51 of the whole angle: twice the error of sine and cosine in fp32 at 31 bits).
 __device__ __forceinline__ void rope_angles(int at, const double* inv_freq, int pairs, float2* cs) {
     for (int p = threadIdx.x & (kWave - 1); p < pairs; p += kWave) {
-        const double turns = (double)at * (inv_freq[p] * 0.15915494309189533577);
+        constexpr double turn = 0.15915494309189535, rest_of_turn = -9.839338337591243e-18;       // 1 / 2 pi
+        const double f = inv_freq[p], step = f * turn, rest = fma(f, rest_of_turn, fma(f, turn, -step));
+        const double whole = rint(at * step);
         float s, c;
-        sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+        sincospif(2.0f * (float)fma((double)at, rest, fma((double)at, step, -whole)), &s, &c);
         cs[p] = float2{c, s};
     }
 }

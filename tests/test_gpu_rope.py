@@ -248,3 +248,35 @@ def test_refused_arguments():
             call(**kw)
         assert e.value.status == status
     torch.cuda.synchronize()
+
+
+def test_far_positions_are_as_accurate_as_near_ones():
+    """Pairs whose first channel all but cancels, so that its bf16 holds the angle's absolute error: at positions of 30 and 31
+    bits as at near ones, in units of 2^-24: 1.6 |(x, y)| for the fraction of a turn in fp32, 2 (|x| + |y|) for sine and
+    cosine, |y| for the first product, and half a step of the result in fp32 and in bf16."""
+    p = need_gpu()
+    T, Hq, R = 600, 2, 64
+    rng = np.random.default_rng(41)
+    pos = np.concatenate((rng.integers(0, 1000, T // 3), rng.integers(2 ** 30, 2 ** 31, T // 3), -rng.integers(2 ** 30, 2 ** 31, T // 3)))
+    freq = rng.uniform(0.5, 1.0, R // 2)
+    angle = pos.astype(np.longdouble)[:, None] * freq.astype(np.longdouble)
+    angle = (angle - np.rint(angle / rope.TWO_PI) * rope.TWO_PI).astype(np.float64)
+    c, s = np.cos(angle)[:, None, :, None], np.sin(angle)[:, None, :, None]
+    # of 128 values x each the one whose nearest y leaves least
+    x = (1 + (np.arange(128) + rng.integers(0, 2)) / 128.0)[None, None, None]
+    y = oq.bf16_to_f32(wl.bf16_bits_from_f32((x * c / s).astype(np.float32))).astype(np.float64)
+    best = np.abs(x * c - y * s).argmin(-1)[..., None]
+    x, y = (np.take_along_axis(np.broadcast_to(v, y.shape), best, -1)[..., 0] for v in (x, y))
+    q = np.concatenate((x, y), -1).repeat(Hq, 1)
+    bits = wl.bf16_bits_from_f32(q.astype(np.float32).reshape(T, Hq * R))
+    k = torch.zeros((T, 1, R), dtype=torch.bfloat16, device="cuda")
+    cache, scale = torch.zeros((0, 1, R), dtype=torch.uint8, device="cuda"), torch.zeros((0, 1), device="cuda")
+    got = p.rope_kv_cache_write(dev_bf16(bits).unflatten(1, (Hq, R)), k, k, dev_i32(pos.astype(np.int32)), torch.from_numpy(freq).cuda(),
+                                torch.zeros(T, dtype=torch.int64, device="cuda"), cache, cache, scale, scale)
+    ref = rope.rotate(q, pos.astype(np.int32), freq, False)[..., :R // 2]
+    x, y = np.abs(q[..., :R // 2]), np.abs(q[..., R // 2:])
+    tol = 2.0 ** -24 * (1.6 * np.hypot(x, y) + 2 * (x + y) + y) + np.abs(ref) * (2.0 ** -8 + 2.0 ** -24)
+    err = np.abs(values(got)[..., :R // 2] - ref)
+    usual = y < 8                                           # (far larger ones stand beside a sine near 0)
+    assert usual.mean() > 0.8 and np.median(np.abs(ref)[usual] / (x + y)[usual]) < 2.0 ** -14
+    assert (err <= tol).all(), (err / tol).max()
