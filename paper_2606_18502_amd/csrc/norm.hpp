@@ -125,9 +125,9 @@ __global__ __launch_bounds__(kNormMaxThreads) void rms_norm_kernel(NormArgs a) {
     });
     block_sum_max(sum, top, red, nw);
     const float cols = (float)a.cols;
-    float r = 1.0f / sqrtf(sum / cols + a.eps), pre = 1.0f;
-    const bool fits = sum < 0x1p126f && r > 0.0f;            // (r = 0: the mean with an eps near the largest number)
+    const bool fits = sum < 0x1p126f && a.eps < 0x1p126f;    // (and the mean with eps)
     const bool plain = fits && top < 0x1p126f;
+    float r = 1.0f / sqrtf(sum / cols + a.eps), pre = 1.0f;
     bool wild = false;                       // an infinite or NaN sum: the row is NaN throughout
     const auto far = [&](float v, float w) { return (float)((double)v * w * ((double)r * pre)); };
     if (plain) {
