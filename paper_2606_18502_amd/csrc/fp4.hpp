@@ -16,9 +16,11 @@
 #pragma once
 
 #include <type_traits>
+#include <utility>
 
 #include "attn_common.hpp"
 #include "kernels.hpp"
+#include "plan.hpp"
 
 namespace specfp8 {
 
@@ -75,7 +77,7 @@ struct Fp4Shape {
     static constexpr int kLoads = NT + kLoadsA;
     static constexpr int kBox = KW > 1 ? KW * kTiles * MT * 1024 : 0;           // the waves' sums
     static constexpr int kScales = KW * D * kStage;                         // of kPanel steps: a word for each and row
-    static constexpr int kPanel = 256 / (kTiles == 1 ? 1 : kTiles == 2 ? 2 : kTiles <= 4 ? 4 : 8);
+    static constexpr int kPanel = fp4_panel(kTiles);
     static constexpr int kPieces = (4 * kTiles * kPanel + kThreads - 1) / kThreads;         // of 16 bytes of scales a thread
     static constexpr int lds(int64_t steps) {
         const int ring = kScales + 16 * kTiles * 4 * ((int)(steps < kPanel ? steps : kPanel) | 1);
@@ -331,6 +333,14 @@ hipError_t launch_fp4_tiles(const Fp4Args& a, hipStream_t stream) {
     return hipGetLastError();
 }
 
+template <size_t... I>
+hipError_t launch_fp4_variant(int at, const Fp4Args& a, hipStream_t stream, std::index_sequence<I...>) {
+    using Launch = hipError_t (*)(const Fp4Args&, hipStream_t);
+    static constexpr Launch launch[] = {launch_fp4_tiles<kFp4Variants[I].mr, kFp4Variants[I].nt, kFp4Variants[I].kw,
+                                                         kFp4Variants[I].nw, kFp4Variants[I].d>...};
+    return launch[at](a, stream);
+}
+
 }  // namespace
 
 hipError_t launch_fp4_quantize(const uint16_t* x, int64_t rows, int64_t cols, int64_t ld_x, uint8_t* q, int64_t ld_q,
@@ -340,55 +350,8 @@ hipError_t launch_fp4_quantize(const uint16_t* x, int64_t rows, int64_t cols, in
     return hipGetLastError();
 }
 
-// The variant, by the workgroups there would be.  Up to one a compute unit, eight waves share K, and a workgroup takes the
-// fewest rows that keep to that number, then two tiles of columns, and above 16 rows 32 of them by two and four: it
-// loads its rows of A and half as many bytes of its columns of W, and few large ones leave compute units idle and load more
-// each.  Beyond that 8 to 64 rows a workgroup (they share a read of W), fewer waves along K and more along the columns,
-// which share A's tile: it is read by every workgroup, and weighs as much as W's does with 16 columns and 8 rows.  Both
-// sides of a border, us, K = 4096 (14336 in brackets; the variant before and after it):
-//   8 rows, 16:  16 by 2048 columns 3.5, 3.5 (6.2, 7.3) -- 4096 4.4, 3.9 (9.5, 8.1)
-//                32 by 1024 3.5, 3.5 (5.7, 6.7) -- 2048 4.4, 3.8 (8.5, 7.3)
-//   two tiles:   5 by 4096 3.4, 4.3 (7.6, 8.5) -- 6144 5.1, 4.7 (10.2, 9.8)
-//                32 by 2048 3.8, 3.9 (7.3, 8.8) -- 4096 5.0, 4.7 (11.1, 9.3)
-//   32 by two:   64 by 2048 4.2, 4.7 (9.1, 11.0) -- 4096 5.9, 5.6 (14.4, 11.8)
-//   by four:     64 by 4096 5.6, 6.6 (11.8, 15.2) -- 6144 7.5, 6.9 (21.9, 15.7)
-//                32 by 8192 6.1, 7.1 (13.1, 16.0) -- 10240 7.8, 7.1 (22.3, 16.7);  16384 8.5, 9.3, with K = 8192 18.8, 14.4
-//   to 8 rows:   8192 5.5, 5.6 (11.7, 11.5) -- 10240 6.4, 6.0 (15.2, 13.5);  12288 6.5, 6.1 (16.6, 19.4) -- 14336 7.4, 7.1
-//                (24.4, 21.8);  16384 7.7, 7.9 (23.9, 24.8) -- 28672 12.4, 11.3
-//   to 16:       8192 5.7, 6.4 (12.0, 14.2) -- 10240 7.0, 6.7 (17.9, 15.9);  16384 8.0, 8.6 -- 28672 12.2, 11.6
-//                28672 11.6, 12.8 -- 57344 27.2, 25.0
-//   to 32:       16384 8.5, 9.3 -- 28672 14.3, 12.5;  28672 12.5, 16.2 -- 57344 30.6, 26.8
-//   more:        64 by 8192 7.3, 9.7 (16.3, 24.0) -- 10240 12.5, 10.0 (30.3, 24.5);  16384 10.9, 11.9 -- 28672 19.3, 15.2
-//                28672 15.2, 16.5 -- 57344 39.6, 32.2
 hipError_t launch_gemm_fp4(const Fp4Args& a, hipStream_t stream) {
-    const int64_t columns = (a.N + 15) / 16;
-    const auto groups = [&](int rows, int64_t of_columns) { return (a.M + rows - 1) / rows * of_columns; };
-    if (groups(8, columns) <= 256) return launch_fp4_tiles<8, 1, 8, 1, 3>(a, stream);
-    if (groups(16, columns) <= 256) return launch_fp4_tiles<16, 1, 8, 1, 3>(a, stream);
-    if (groups(16, (columns + 1) / 2) <= 256)
-        return a.M <= 8 ? launch_fp4_tiles<8, 2, 8, 1, 2>(a, stream) : launch_fp4_tiles<16, 2, 8, 1, 2>(a, stream);
-    const int64_t tiles = groups(64, columns);
-    if (a.M <= 8) {
-        if (tiles <= 768) return launch_fp4_tiles<8, 1, 4, 1, 3>(a, stream);
-        if (tiles <= 1024) return launch_fp4_tiles<8, 2, 4, 1, 3>(a, stream);
-        return launch_fp4_tiles<8, 2, 4, 1, 2>(a, stream);
-    }
-    if (a.M <= 16) {
-        if (tiles <= 1024) return launch_fp4_tiles<16, 2, 4, 1, 2>(a, stream);
-        if (tiles <= 2048) return launch_fp4_tiles<16, 4, 4, 1, 2>(a, stream);
-        return launch_fp4_tiles<16, 4, 2, 2, 3>(a, stream);
-    }
-    if (groups(32, (columns + 1) / 2) <= 256) return launch_fp4_tiles<32, 1, 4, 2, 3>(a, stream);
-    const int64_t fours = groups(32, (columns + 3) / 4);
-    if (fours <= 256 && (a.M > 32 || a.K > 8192 || fours <= 192)) return launch_fp4_tiles<32, 2, 4, 2, 3>(a, stream);
-    if (a.M <= 32) {
-        if (tiles <= 1024) return launch_fp4_tiles<32, 1, 4, 2, 3>(a, stream);
-        if (tiles <= 2048) return launch_fp4_tiles<32, 1, 2, 4, 3>(a, stream);
-        return launch_fp4_tiles<32, 4, 2, 2, 2>(a, stream);
-    }
-    if (tiles <= 1024) return launch_fp4_tiles<64, 1, 2, 4, 3>(a, stream);
-    if (tiles <= 2048) return launch_fp4_tiles<64, 1, 1, 4, 3>(a, stream);
-    return launch_fp4_tiles<64, 1, 1, 8, 3>(a, stream);
+    return launch_fp4_variant(plan_fp4(a.M, a.N, a.K), a, stream, std::make_index_sequence<kFp4VariantCount>());
 }
 
 }  // namespace specfp8

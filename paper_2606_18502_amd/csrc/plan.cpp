@@ -226,4 +226,54 @@ size_t paged_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t
     return plan_paged(T, B, Hq, H, D, 2147483647).bytes;
 }
 
+// The variant, by the workgroups there would be.  Up to one a compute unit, eight waves share K, and a workgroup takes the
+// fewest rows that keep to that number, then two tiles of columns, and above 16 rows 32 of them by two and four: it
+// loads its rows of A and half as many bytes of its columns of W, and few large ones leave compute units idle and load more
+// each.  Beyond that 8 to 64 rows a workgroup (they share a read of W), fewer waves along K and more along the columns,
+// which share A's tile: it is read by every workgroup, and weighs as much as W's does with 16 columns and 8 rows.  Both
+// sides of a border, us, K = 4096 (14336 in brackets; the variant before and after it):
+//   8 rows, 16:  16 by 2048 columns 3.5, 3.5 (6.2, 7.3) -- 4096 4.4, 3.9 (9.5, 8.1)
+//                32 by 1024 3.5, 3.5 (5.7, 6.7) -- 2048 4.4, 3.8 (8.5, 7.3)
+//   two tiles:   5 by 4096 3.4, 4.3 (7.6, 8.5) -- 6144 5.1, 4.7 (10.2, 9.8)
+//                32 by 2048 3.8, 3.9 (7.3, 8.8) -- 4096 5.0, 4.7 (11.1, 9.3)
+//   32 by two:   64 by 2048 4.2, 4.7 (9.1, 11.0) -- 4096 5.9, 5.6 (14.4, 11.8)
+//   by four:     64 by 4096 5.6, 6.6 (11.8, 15.2) -- 6144 7.5, 6.9 (21.9, 15.7)
+//                32 by 8192 6.1, 7.1 (13.1, 16.0) -- 10240 7.8, 7.1 (22.3, 16.7);  16384 8.5, 9.3, with K = 8192 18.8, 14.4
+//   to 8 rows:   8192 5.5, 5.6 (11.7, 11.5) -- 10240 6.4, 6.0 (15.2, 13.5);  12288 6.5, 6.1 (16.6, 19.4) -- 14336 7.4, 7.1
+//                (24.4, 21.8);  16384 7.7, 7.9 (23.9, 24.8) -- 28672 12.4, 11.3
+//   to 16:       8192 5.7, 6.4 (12.0, 14.2) -- 10240 7.0, 6.7 (17.9, 15.9);  16384 8.0, 8.6 -- 28672 12.2, 11.6
+//                28672 11.6, 12.8 -- 57344 27.2, 25.0
+//   to 32:       16384 8.5, 9.3 -- 28672 14.3, 12.5;  28672 12.5, 16.2 -- 57344 30.6, 26.8
+//   more:        64 by 8192 7.3, 9.7 (16.3, 24.0) -- 10240 12.5, 10.0 (30.3, 24.5);  16384 10.9, 11.9 -- 28672 19.3, 15.2
+//                28672 15.2, 16.5 -- 57344 39.6, 32.2
+int plan_fp4(int64_t M, int64_t N, int64_t K) {
+    const int64_t columns = (N + 15) / 16;
+    const auto groups = [&](int rows, int64_t of_columns) { return (M + rows - 1) / rows * of_columns; };
+    if (groups(8, columns) <= 256) return kFp4<8, 1, 8, 1, 3>;
+    if (groups(16, columns) <= 256) return kFp4<16, 1, 8, 1, 3>;
+    if (groups(16, (columns + 1) / 2) <= 256) return M <= 8 ? kFp4<8, 2, 8, 1, 2> : kFp4<16, 2, 8, 1, 2>;
+    const int64_t tiles = groups(64, columns);
+    if (M <= 8) {
+        if (tiles <= 768) return kFp4<8, 1, 4, 1, 3>;
+        if (tiles <= 1024) return kFp4<8, 2, 4, 1, 3>;
+        return kFp4<8, 2, 4, 1, 2>;
+    }
+    if (M <= 16) {
+        if (tiles <= 1024) return kFp4<16, 2, 4, 1, 2>;
+        if (tiles <= 2048) return kFp4<16, 4, 4, 1, 2>;
+        return kFp4<16, 4, 2, 2, 3>;
+    }
+    if (groups(32, (columns + 1) / 2) <= 256) return kFp4<32, 1, 4, 2, 3>;
+    const int64_t fours = groups(32, (columns + 3) / 4);
+    if (fours <= 256 && (M > 32 || K > 8192 || fours <= 192)) return kFp4<32, 2, 4, 2, 3>;
+    if (M <= 32) {
+        if (tiles <= 1024) return kFp4<32, 1, 4, 2, 3>;
+        if (tiles <= 2048) return kFp4<32, 1, 2, 4, 3>;
+        return kFp4<32, 4, 2, 2, 2>;
+    }
+    if (tiles <= 1024) return kFp4<64, 1, 2, 4, 3>;
+    if (tiles <= 2048) return kFp4<64, 1, 1, 4, 3>;
+    return kFp4<64, 1, 1, 8, 3>;
+}
+
 }  // namespace specfp8

@@ -97,6 +97,30 @@ constexpr int64_t kAcceptSlice = (int64_t)64 * kAcceptVecs * 8;          // 4096
 constexpr int kAcceptPerThread = kAcceptVecs * 8;                        // 64 logits per thread (sampling)
 constexpr int64_t kAcceptChunk = (int64_t)kAcceptThreads * kAcceptPerThread;   // 16384 logits per sampling block
 
+// ---- 4-bit linears --------------------------------------------------------------
+// A kernel: rows of A and tiles of 16 columns a wave, waves along K and along the columns, stages of a ring (fp4.hpp).
+struct Fp4Variant {
+    int mr, nt, kw, nw, d;
+    constexpr bool operator==(const Fp4Variant& o) const {
+        return mr == o.mr && nt == o.nt && kw == o.kw && nw == o.nw && d == o.d;
+    }
+};
+constexpr Fp4Variant kFp4Variants[] = {
+    {8, 1, 8, 1, 3}, {16, 1, 8, 1, 3}, {8, 2, 8, 1, 2}, {16, 2, 8, 1, 2}, {8, 1, 4, 1, 3}, {8, 2, 4, 1, 3},
+    {8, 2, 4, 1, 2}, {16, 2, 4, 1, 2}, {16, 4, 4, 1, 2}, {16, 4, 2, 2, 3}, {32, 1, 4, 2, 3}, {32, 2, 4, 2, 3},
+    {32, 1, 2, 4, 3}, {32, 4, 2, 2, 2}, {64, 1, 2, 4, 3}, {64, 1, 1, 4, 3}, {64, 1, 1, 8, 3}};
+constexpr int kFp4VariantCount = sizeof(kFp4Variants) / sizeof(kFp4Variants[0]);
+constexpr int fp4_index(Fp4Variant v) {      // (one that is not listed does not compile)
+    int i = 0;
+    while (!(kFp4Variants[i] == v)) ++i;
+    return i;
+}
+template <int... V>
+constexpr int kFp4 = fp4_index(Fp4Variant{V...});
+// Steps of 128 k whose scales a workgroup of so many tiles holds at a time.
+constexpr int fp4_panel(int tiles) { return 256 / (tiles == 1 ? 1 : tiles == 2 ? 2 : tiles <= 4 ? 4 : 8); }
+int plan_fp4(int64_t M, int64_t N, int64_t K);           // which of kFp4Variants
+
 // ---- rotation into the cache ----------------------------------------------------
 constexpr int64_t kRopeStep = 1 << 24;       // items (parts of tokens) that a grid's waves take at a time, counted in 32 bits
 

@@ -10,6 +10,7 @@ import torch
 
 import workloads as wl
 from oracle import e4m3, fp4, gemm as og, quantize as oq
+from tests import fp4_cases
 from tests.gpu_util import dev_bf16, dev_f32, dev_u8, host, host_bf16_bits, need_gpu, say
 
 pytestmark = pytest.mark.gpu
@@ -200,3 +201,18 @@ def test_refused_arguments():
     assert e.value.status == 3
     assert p.gemm_fp4(a[:0], sa[:0], w, sw).shape == (0, 8)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("v,M,N,K", fp4_cases.beyond_panels())
+def test_every_variant_beyond_a_panel_of_scales(v, M, N, K):
+    """Scales, ring and pointers go on in a second and third panel; some waves have no step there, and K ends inside one."""
+    p = need_gpu()
+    say(f"gemm_fp4 panels variant={v} M={M} N={N} K={K}")
+    rng = np.random.default_rng(N + K)
+    a, sa = oq.quantize_rows(wl.linear_activations(M, K, 1, 0.01, 20.0))
+    w = rng.integers(0, 256, (N, K // 2), dtype=np.uint8)
+    sw = rng.integers(120, 128, (N, K // 32), dtype=np.uint8)
+    d = dev_u8(a), dev_f32(sa), dev_u8(w), dev_u8(sw)
+    cols = np.unique(np.concatenate((rng.choice(N, 24), np.arange(17), np.arange(N - 17, N))))
+    y32, y16 = p.gemm_fp4(*d, out_dtype=torch.float32), p.gemm_fp4(*d)
+    check(y32[:, cols].contiguous(), y16[:, cols].contiguous(), a, sa, w[cols], sw[cols])
