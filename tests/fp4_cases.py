@@ -24,3 +24,14 @@ def beyond_panels():
         if N * K < 400_000_000:
             out.append((v, M, N, K))
     return out
+
+
+# N, K and numbers of rows of A that one variant serves
+ROWS = [
+    (300, 4128, (8, 1, 8, 1, 3), (1, 7, 8)), (2500, 1056, (16, 1, 8, 1, 3), (9, 12, 16)), (6144, 4128, (8, 2, 8, 1, 2), (1, 5, 8)),
+    (6144, 4128, (16, 2, 8, 1, 2), (9, 10, 16)), (6144, 4128, (32, 1, 4, 2, 3), (17, 25, 32)), (6144, 4128, (32, 2, 4, 2, 3), (33, 50, 64)),
+    (6144, 4128, (64, 1, 2, 4, 3), (65, 80, 128)), (9000, 1056, (8, 1, 4, 1, 3), (1, 8)), (9000, 1056, (16, 2, 4, 1, 2), (9, 16)),
+    (14000, 1056, (8, 2, 4, 1, 3), (1, 3, 8)), (17000, 1056, (8, 2, 4, 1, 2), (1, 8)), (17000, 1056, (16, 4, 4, 1, 2), (9, 16)),
+    (17000, 1056, (32, 1, 2, 4, 3), (17, 32)), (17000, 1056, (64, 1, 1, 4, 3), (33, 64)), (17000, 1056, (64, 1, 1, 8, 3), (65, 100, 128)),
+    (33011, 1056, (16, 4, 2, 2, 3), (9, 16)), (33011, 1056, (32, 4, 2, 2, 2), (17, 32)),
+]

@@ -216,3 +216,20 @@ def test_every_variant_beyond_a_panel_of_scales(v, M, N, K):
     cols = np.unique(np.concatenate((rng.choice(N, 24), np.arange(17), np.arange(N - 17, N))))
     y32, y16 = p.gemm_fp4(*d, out_dtype=torch.float32), p.gemm_fp4(*d)
     check(y32[:, cols].contiguous(), y16[:, cols].contiguous(), a, sa, w[cols], sw[cols])
+
+
+@pytest.mark.parametrize("N,K,v,counts", fp4_cases.ROWS)
+def test_a_row_has_the_same_bits_among_all_counts_of_a_variant(N, K, v, counts):
+    """First and last rows alone among fewer: a variant's rows do not see each other."""
+    p = need_gpu()
+    say(f"gemm_fp4 rows variant={v} N={N} K={K}")
+    most = counts[-1]
+    rng = np.random.default_rng(N + most)
+    a, sa = oq.quantize_rows(wl.linear_activations(most, K, 3, 0.01, 20.0))
+    w = rng.integers(0, 256, (N, K // 2), dtype=np.uint8)
+    sw = rng.integers(120, 128, (N, K // 32), dtype=np.uint8)
+    d = dev_u8(a), dev_f32(sa), dev_u8(w), dev_u8(sw)
+    whole = p.gemm_fp4(*d, out_dtype=torch.float32)
+    for m in counts:
+        for rows in (slice(0, m), slice(most - m, most)):
+            assert torch.equal(p.gemm_fp4(d[0][rows], d[1][rows], d[2], d[3], out_dtype=torch.float32), whole[rows]), (m, rows)

@@ -69,3 +69,9 @@ def test_the_4_bit_linears_have_no_other_variants(plan):
     seen = {fp4(plan, M, N, K)[0] for M in (*range(1, 140), 1000, (1 << 20) - 16) for N in (*range(8, 40000, 347), 128256, (1 << 28) - 1)
             for K in (32, 4096, 8192, 8224, 1 << 30)}
     assert seen == set(fp4_cases.VARIANTS)
+
+
+def test_each_group_of_rows_takes_the_variant_it_names(plan):
+    for N, K, want, rows in fp4_cases.ROWS:
+        assert {fp4(plan, M, N, K)[0] for M in range(rows[0], rows[-1] + 1)} == {want}, (N, K, rows)
+    assert {v for _, _, v, _ in fp4_cases.ROWS} == set(fp4_cases.VARIANTS)
