@@ -231,7 +231,7 @@ spec_status spec_fp8_kv_cache_write(const void* k, int64_t ld_k, const void* v, 
  *
  *   (x cos f - y sin f, y cos f + x sin f),   f = positions[t] * inv_freq[i]
  *
- * in fp32, with f in 64 bits and reduced to one turn there; channels from R on stay
+ * in fp32, with f reduced to one turn in 64 bits; channels from R on stay
  * as they are.  Any scheme that stretches positions is a choice of inv_freq.
  *
  *   q_out[t] = bf16_RNE(rotated q[t])
@@ -246,7 +246,8 @@ spec_status spec_fp8_kv_cache_write(const void* k, int64_t ld_k, const void* v, 
  * k, v     bf16 [T, ld_k] / [T, ld_v], H heads of D; the column blocks of the QKV projection's output fit directly.
  * q_out, k_out  bf16 [T, ld_q_out] / [T, ld_k_out]; may be q and k themselves (same pointer and stride), and
  *          overlap no input otherwise.  Columns behind the heads keep their contents.
- * positions int32 [T]; inv_freq fp64 [R/2], finite (of magnitude at most 1 or so: the angle is exact to 2^-52 of itself).
+ * positions int32 [T]; inv_freq fp64 [R/2], finite (of magnitude at most 1 or so: f is then within some 2^-51 radians, besides
+ *          whole turns, at every position, before its sine and cosine are taken in fp32).
  * slot_mapping, num_slots, mode, k_scale, v_scale, k_cache, v_cache: as spec_fp8_kv_cache_write.
  * Requirements: those of spec_fp8_kv_cache_write; Hq >= 0, 0 < R <= D, ld_q and ld_q_out >= Hq*D, ld_k_out >= H*D
  * (SPEC_ERR_SHAPE); R % 8 == 0, Hq and H <= 65535, strides < 2^35 (SPEC_ERR_UNSUPPORTED); q, q_out and k_out 16-byte aligned, their strides
@@ -360,7 +361,8 @@ spec_status spec_fp4_quantize(const void* x, int64_t rows, int64_t cols, int64_t
  * Y       bf16 or fp32 [M, ldy], N <= ldy.
  * Products are exact; the matrix cores' sums are those of spec_fp8_gemm.  The order of summation depends on N, K and M
  * alone.  No workspace.
- * Any M is computed, but at most 64 rows share a read of the weights: for many rows spec_fp8_gemm is made.
+ * Any M is computed, but at most 64 rows share a read of the weights, and times grow with M beyond that; spec_fp8_gemm is
+ * made for many rows, but of E4M3 weights, which nothing here makes from 4-bit ones: a program with both would hold both.
  * Requirements: M >= 0 (0 is a no-op), N > 0, K > 0, lda >= K, ldw >= K/2, ld_w_scale >= K/32, ldy >= N (SPEC_ERR_SHAPE);
  * K % 32 == 0, K <= 2^30, N < 2^28, M <= 2^20 - 16 (SPEC_ERR_UNSUPPORTED); A, W and Y 16-byte aligned, lda and ldw
  * multiples of 16, ldy of 8, a_scale 4-byte aligned (w_scale takes any stride and address) (SPEC_ERR_ALIGN).

@@ -8,11 +8,12 @@
 // A lane group g = lane / 16 of the weights' operand holds k 32 g .. of a row and applies the scale byte that it
 // brings to them; of the activations' operand k 16 g .. and 64 + 16 g .. of a column.
 //
-// What bounds it: W's bytes.  8 rows by 128256 x 4096 take 51.7 us (5.4 TB/s of 279 MB; a read of a large array 5.8),
-// 5 by 4096 x 14336 7.7 and 1 by 6144 x 4096 4.8, of which 2.2 a launch.  With 64 rows A counts, too: every workgroup
-// reads its rows of it (64 by 28672 x 4096 15.1 us, 62 MB of W; 64 by 4096 x 14336 11.8 us, 117 MB of A and 59 of W for
-// 29 in memory), and from LDS each wave.  Operands straight from memory to registers took 94, 11.6, 5.9 and 66 us for the
-// first four: 16 rows a load instruction in the matrix cores' order of lanes, and scales word by word.
+// What bounds it: W's bytes.  8 rows by 128256 x 4096 take 51.8 us (5.4 TB/s of 279 MB; a read of a large array 5.8).
+// Smaller weights that were read a short while ago come from the Infinity Cache: 5 by 4096 x 14336 7.4 us, from memory 8.9;
+// 1 by 6144 x 4096 4.7 and 5.9, of which 2.2 a launch.  With 64 rows A counts, too: every workgroup
+// reads its rows of it (64 by 28672 x 4096 16.1 us, from memory 21.5, 62 MB of W; 64 by 4096 x 14336 12.0 and 16.6, 117 MB
+// of A and 59 of W for 29 in memory), and from LDS each wave.  Operands straight from memory to registers took 94, 11.6, 5.9
+// and 66 us for the first four (weights in the cache where they fit): 16 rows a load instruction in the matrix cores' order of lanes, and scales word by word.
 #pragma once
 
 #include <type_traits>

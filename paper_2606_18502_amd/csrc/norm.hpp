@@ -6,8 +6,9 @@
 //
 // One workgroup owns a row and keeps its sums in registers (rows of up to 32768 channels): every input is read once, every
 // output written once.  What bounds it: memory for many rows (8191 x 4096 with residual and codes 41 us, 5.7 TB/s of
-// 235 MB; a large copy runs at 5.1), a launch and two round trips for few (1 x 4096 3.1 us, of which 2.2 a launch).
-// 1000 x 65536 take 126 us (3.6 TB/s of what has to move): read twice.
+// 235 MB; a large copy runs at 5.1), a launch and two round trips for few (1 x 4096 2.6 us, of which 2.2 a launch).
+// 1000 x 65536 take 126 us (3.6 TB/s of what has to move): read twice.  Rows whose squares or products exceed fp32 sum them
+// scaled and take y from 64 bits; the test for them costs nothing that shows (320 x 4096 in a graph 3.85 us, without 3.86).
 #pragma once
 
 #include "device_common.hpp"

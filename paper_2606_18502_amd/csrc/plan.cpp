@@ -231,7 +231,8 @@ size_t paged_attention_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t
 // loads its rows of A and half as many bytes of its columns of W, and few large ones leave compute units idle and load more
 // each.  Beyond that 8 to 64 rows a workgroup (they share a read of W), fewer waves along K and more along the columns,
 // which share A's tile: it is read by every workgroup, and weighs as much as W's does with 16 columns and 8 rows.  Both
-// sides of a border, us, K = 4096 (14336 in brackets; the variant before and after it):
+// sides of a border, us, K = 4096 (14336 in brackets; the variant before and after it), a few sets of operands in turn, so that
+// weights below some 80 MB came from the Infinity Cache:
 //   8 rows, 16:  16 by 2048 columns 3.5, 3.5 (6.2, 7.3) -- 4096 4.4, 3.9 (9.5, 8.1)
 //                32 by 1024 3.5, 3.5 (5.7, 6.7) -- 2048 4.4, 3.8 (8.5, 7.3)
 //   two tiles:   5 by 4096 3.4, 4.3 (7.6, 8.5) -- 6144 5.1, 4.7 (10.2, 9.8)

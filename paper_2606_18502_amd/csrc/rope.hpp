@@ -1,8 +1,8 @@
 // The position rotation of new queries and keys on the way into the paged FP8 cache.
 //
-// Mathematics.  Pair i of a head's first R channels turns by angle position * inv_freq[i].  The angle is taken in
-// 64 bits and in turns (position * inv_freq / 2 pi, its whole turns dropped), so that positions far into a context keep
-// the accuracy of the first; sine and cosine of the rest, and the rotation, are fp32.  Keys are quantized from the
+// Mathematics.  Pair i of a head's first R channels turns by angle position * inv_freq[i].  The angle is taken in turns
+// (position * inv_freq / 2 pi, its whole turns dropped) with the second factor in two parts of 64 bits, so that positions of
+// 31 bits keep the accuracy of the first; sine and cosine of the rest, and the rotation, are fp32.  Keys are quantized from the
 // rotated fp32 values, values as the plain cache write does it.
 //
 // A wave takes a token, or one of 2^log_parts parts of its rows (query heads, key heads, value heads): it evaluates the
@@ -10,8 +10,9 @@
 // channels each: VEC of the lower and VEC of the upper half of the rotated channels, or 2 VEC side by side where
 // neighbours turn together and where nothing turns.
 //
-// What bounds it: memory for many tokens (8191 of 32 + 2 x 8 heads of 128, keys as bf16 too: 43.8 us, 4.6 TB/s of 202 MB;
-// a large copy runs at 5.1), a launch and three round trips for few (1 token 3.5 us, 320 4.4, of which 2.2 a launch).
+// What bounds it: memory for many tokens (8191 of 32 + 2 x 8 heads of 128, keys as bf16 too: 43.6 us, 4.6 TB/s of 202 MB;
+// a large copy runs at 5.1), a launch and three round trips one after the other for few (1 token 3.3 us, 320 4.7, of which
+// 2.2 a launch): slot and position, then inv_freq, then, behind the exchange of angles, the rows.
 // Not faster there: the next rows loaded under this one's arithmetic (47.5), more waves a SIMD (45.4 and 52.8), workgroups
 // of 2 or 8 waves.  Stores past the caches gain 2 to 4 us here, and the attention that reads q next loses them.
 #pragma once

@@ -75,7 +75,8 @@ def rms_norm_quantize(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-5,
 
     x, weight, residual, residual_out: as for rms_norm.  Dynamic per-row scales unless
     `per_tensor_scale` (fp32 [1]) is given.  normed: bf16 [rows, cols] that also receives the
-    normed values, or None.
+    normed values, or None.  scales: fp32 [rows] that receives the per-row scales, or None; not looked at with
+    `per_tensor_scale`.
     Returns (codes uint8 [rows, cols], scales fp32 [rows] or the given [1], residual_out or None).
     """
     return (_bind or _load_bind()).rms_norm_quantize(x, weight, eps, residual, per_tensor_scale, residual_out, normed, out,
@@ -215,7 +216,8 @@ def gemm_fp4(a: torch.Tensor, sa: torch.Tensor, w: torch.Tensor, sw: torch.Tenso
     """Y = dec(A) dec4(W)^T * sa with 4-bit weights, for few rows (spec_fp8_gemm_fp4).
 
     a: uint8 E4M3 [M, K]; sa: fp32 [M] (per token) or [1] (per tensor); w: uint8 [N, K/2] and
-    sw: uint8 [N, K/32] of quantize_fp4.  At most 64 rows of a share a read of the weights: for many rows, gemm.
+    sw: uint8 [N, K/32] of quantize_fp4.  At most 64 rows of a share a read of the weights
+    (gemm, made for many rows, takes E4M3 weights).
     """
     f32 = True if out_dtype is torch.float32 else (False if out_dtype is torch.bfloat16 else None)
     return (_bind or _load_bind()).gemm_fp4(a, sa, w, sw, f32, out)
